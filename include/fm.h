@@ -234,6 +234,65 @@ int fm_stratified_end(fm_matrix* m, const fm_params* p, float* w0, void* hip_str
 int fm_get_aux(const fm_matrix* m, float* a /*N*/, float* G /*N*K*/, float* q /*N*/, float* r /*N*/,
                void* hip_stream);
 
+/* ---- the candidates of a field: serving and distillation ----
+ * A field is a block of C columns of which a row has one (the next item, the next term).  A row that holds everything
+ * but that field, with aggregates G_i from fm_forward, scores candidate j of it (value 1) as
+ *     z_ij = w_j + sum_k G_ik v_jk
+ * plus a part that is the same for all candidates, so the model of the field is the softmax of scale * z_i:
+ *     lse_i = log sum_j exp(scale z_ij),   log p_ij = scale z_ij - lse_i      (sums over the allowed candidates)
+ * Candidates are numbered 0..C-1 from the first row of V and the first entry of w on; V + first * K and w + first make a
+ * field of a block of columns.  A candidate is allowed in a row if its bit in the row's mask is set (all are without a mask)
+ * and its logit is above -infinity; whatever stands in V and w at candidates that no row allows is not part of any result.
+ * The logits are never stored: n and C may be such that n C values would not fit.  Sums and probabilities are fp32.
+ * A row with an allowed logit that is NaN or +infinity gets NaN for all of its values (top_ids -1).
+ *
+ * The handle holds workspace for calls of up to max_rows rows and max_top best candidates (0..64), on the device that is
+ * current when it is made.  Calls allocate nothing, never wait for the stream and may be captured into a graph; two calls
+ * on one handle must not overlap in time.  1 <= C < 2^31, K as in fm_params, 1 <= max_rows < 2^31. */
+typedef struct fm_field fm_field;
+
+typedef enum { FM_TYPE_F32 = 0, FM_TYPE_F16 = 1 /* IEEE binary16 */, FM_TYPE_BF16 = 2 } fm_type;
+
+/* What the rows choose from.  V and w are read in the call: they may change from call to call. */
+typedef struct {
+    const void* V;        /* DEVICE, C rows of K values of v_type, aligned like one value */
+    const float* w;       /* DEVICE C, nullable (zeros) */
+    const uint32_t* mask; /* DEVICE, nullable: candidate j in bit j % 32 of word j / 32 */
+    int64_t v_stride;     /* values from one row of V to the next, >= K */
+    int64_t mask_stride;  /* words from one row's mask to the next, >= ceil(C / 32); 0: one mask for all rows */
+    int32_t v_type;       /* fm_type */
+    float scale;          /* 1 / temperature, positive and finite */
+} fm_candidates;
+
+int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t max_top, fm_field** out);
+int fm_field_destroy(fm_field* f);
+const char* fm_field_last_error(const fm_field* f); /* f may be NULL: last creation error of this thread */
+
+/* Log probabilities of n rows (G: DEVICE, fp32, g_stride values from one row to the next, aligned like one value).
+ * Any DEVICE output may be NULL.
+ *   logprob[i T + t] = log p of candidate ids[i T + t]; 0 where that is outside [0, C); -infinity where it is not allowed
+ *   lse[i], entropy[i] = -sum_j p_ij log p_ij (in nats)
+ *   top_ids[i top + a], top_logprob[i top + a]: the a-th best allowed candidate, by z descending, lower numbers first among
+ *     equal ones; -1 and -infinity from where the row has no more
+ * A row with no allowed candidate has lse -infinity and entropy 0. */
+int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride, int32_t T,
+                      const int32_t* ids /*DEVICE n*T*/, float* logprob /*DEVICE n*T*/, float* lse /*DEVICE n*/,
+                      float* entropy /*DEVICE n*/, int32_t top, int32_t* top_ids /*DEVICE n*top*/,
+                      float* top_logprob /*DEVICE n*top*/, void* hip_stream);
+
+/* Distillation from a teacher's T largest logits of every row, T >= 1; entries with ids outside [0, C) and such that the
+ * row does not allow are left out, the ids of a row are distinct (the shares of equal ones add up).
+ *   q_it   = softmax over the entries of a row of scale * teacher_it
+ *   loss_i = sum_t q_it (log q_it - log p_{i, ids_it})               (Kullback-Leibler; T = 1: cross entropy of a label)
+ * and the gradient of sum_i weight_i loss_i (weight NULL: ones), with d_ij = weight_i scale (p_ij - q_ij):
+ *   grad_G_i = sum_j d_ij v_j,   grad_V_j = sum_i d_ij G_i,   grad_w_j = sum_i d_ij          (fp32, contiguous, overwritten)
+ * A row without entries or without allowed candidates has loss 0 and takes no part in the gradient, nor does one of
+ * weight 0.  Any DEVICE output may be NULL. */
+int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride, int32_t T,
+                     const int32_t* ids /*DEVICE n*T*/, const float* teacher /*DEVICE n*T*/,
+                     const float* weight /*DEVICE n*/, float* loss /*DEVICE n*/, float* grad_G /*DEVICE n*K*/,
+                     float* grad_V /*DEVICE C*K*/, float* grad_w /*DEVICE C*/, void* hip_stream);
+
 /* Per-kernel timing with HIP events on the launch stream.  While enabled, every kernel
  * launch of this handle is bracketed by two events, and kernels that normally overlap on
  * internal side streams run back to back on the launch stream, so that each is timed alone.

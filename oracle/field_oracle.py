@@ -1,0 +1,87 @@
+"""The candidates of a field in 64 bits, row by row from the definitions (numpy; test infrastructure only).
+
+Row i with aggregates G_i scores candidate j as z_ij = w_j + <G_i, v_j>; its model of the field is the softmax of
+scale * z_i over the allowed candidates."""
+import numpy as np
+
+
+def logits(G, V, w=None, allowed=None):
+    """z [n x C]; -inf where a candidate is not allowed (allowed: truth values, [C] or [n x C])."""
+    G, V = np.asarray(G, np.float64), np.asarray(V, np.float64)
+    with np.errstate(invalid="ignore"):
+        z = np.stack([V @ g for g in G]) if len(G) else np.zeros((0, len(V)))
+        if w is not None:
+            z = z + np.asarray(w, np.float64)[None, :]
+    if allowed is not None:
+        z = np.where(np.broadcast_to(allowed, z.shape), z, -np.inf)
+    return z
+
+
+def log_softmax(z, scale=1.0):
+    """(log p, lse) of every row: -inf where z is, NaN throughout a row with a NaN or +inf."""
+    logp, lse = np.full(z.shape, -np.inf), np.full(len(z), -np.inf)
+    for i, row in enumerate(z):
+        if np.isnan(row).any() or np.isposinf(row).any():
+            logp[i], lse[i] = np.nan, np.nan
+            continue
+        live = row > -np.inf
+        if live.any():
+            x = scale * row[live]
+            m = x.max()
+            lse[i] = m + np.log(np.exp(x - m).sum())
+            logp[i, live] = x - lse[i]
+    return logp, lse
+
+
+def logprobs(z, scale=1.0, ids=None, top=0):
+    logp, lse = log_softmax(z, scale)
+    n, C = z.shape
+    out = dict(lse=lse, entropy=np.zeros(n))
+    for i in range(n):
+        live = logp[i] > -np.inf
+        out["entropy"][i] = np.nan if np.isnan(lse[i]) else -(np.exp(logp[i, live]) * logp[i, live]).sum()
+    if ids is not None:
+        out["logprob"] = np.array([[logp[i, j] if 0 <= j < C else 0.0 for j in row] for i, row in enumerate(ids)])
+    if top:
+        out["top_ids"], out["top_logprob"] = np.full((n, top), -1, np.int32), np.full((n, top), -np.inf)
+        for i in range(n):
+            if np.isnan(lse[i]):
+                out["top_logprob"][i] = np.nan
+                continue
+            best = [j for j in np.lexsort((np.arange(C), -z[i])) if z[i, j] > -np.inf][:top]
+            out["top_ids"][i, :len(best)] = best
+            out["top_logprob"][i, :len(best)] = logp[i, best]
+    return out
+
+
+def teacher_softmax(z, scale, ids, teacher):
+    """q [n x T]: 0 for entries that are left out."""
+    n, C = z.shape
+    q = np.zeros(np.shape(teacher))
+    for i in range(n):
+        ok = [t for t, j in enumerate(ids[i]) if 0 <= j < C and not z[i, j] == -np.inf]
+        if ok:
+            x = scale * np.asarray(teacher[i], np.float64)[ok]
+            e = np.exp(x - x.max())
+            q[i, ok] = e / e.sum()
+    return q
+
+
+def distill(z, G, V, scale, ids, teacher, weight=None):
+    """Loss of every row, the gradient of sum_i weight_i loss_i, and d = its derivative by the logits."""
+    G, V = np.asarray(G, np.float64), np.asarray(V, np.float64)
+    n, C = z.shape
+    logp, _ = log_softmax(z, scale)
+    q = teacher_softmax(z, scale, ids, teacher)
+    loss, d = np.zeros(n), np.zeros((n, C))
+    for i in range(n):
+        if not (q[i] > 0).any():
+            continue
+        for t in np.flatnonzero(q[i]):
+            loss[i] += q[i, t] * (np.log(q[i, t]) - logp[i, ids[i][t]])
+        g = scale * (1.0 if weight is None else float(weight[i]))
+        if g != 0:
+            d[i] = g * np.exp(logp[i])
+            np.subtract.at(d[i], np.asarray(ids[i])[q[i] > 0], g * q[i][q[i] > 0])
+    product = lambda a, b: np.stack([(r[r != 0, None] * b[r != 0]).sum(0) for r in a]) if len(a) else np.zeros((0, b.shape[1]))  # noqa: E731
+    return dict(loss=loss, grad_G=product(d, V), grad_V=product(d.T, G), grad_w=d.sum(0), d=d, q=q)

@@ -15,6 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libfm_mi355x.so")
 FM_OK = 0
 FM_LOSS_SQUARED = 0
 FM_LOSS_LOGISTIC = 1
+FM_TYPE_F32, FM_TYPE_F16, FM_TYPE_BF16 = 0, 1, 2
 FM_EINVAL, FM_ENOMEM, FM_EUNSORTED, FM_ERANGE, FM_ESTATE, FM_EHIP = -1, -2, -3, -4, -5, -6
 STATUS_NAMES = {FM_OK: "FM_OK", FM_EINVAL: "FM_EINVAL", FM_ENOMEM: "FM_ENOMEM", FM_EUNSORTED: "FM_EUNSORTED",
                 FM_ERANGE: "FM_ERANGE", FM_ESTATE: "FM_ESTATE", FM_EHIP: "FM_EHIP"}
@@ -29,6 +30,12 @@ class fm_params(ctypes.Structure):
                 ("half_gather", ctypes.c_int32)]
 
 
+class fm_candidates(ctypes.Structure):
+    _fields_ = [("V", ctypes.c_void_p), ("w", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("v_stride", ctypes.c_int64), ("mask_stride", ctypes.c_int64),
+                ("v_type", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class FMError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"{STATUS_NAMES.get(code, code)}: {msg}")
@@ -41,7 +48,8 @@ EXPORTS = ["fm_build_csr", "fm_build_csc", "fm_partition", "fm_partition_placed"
            "fm_sgd_epoch", "fm_minibatch_epoch", "fm_stratified_epoch", "fm_stratified_begin", "fm_stratified_step",
            "fm_stratified_end", "fm_get_aux", "fm_profile_enable", "fm_profile_kernels",
            "fm_profile_kernel_name", "fm_profile_read", "fm_set_option", "fm_set_tuning", "fm_set_tile_tuning", "fm_destroy",
-           "fm_trim", "fm_last_error"]
+           "fm_trim", "fm_last_error", "fm_field_create", "fm_field_destroy", "fm_field_last_error", "fm_field_logprobs",
+           "fm_field_distill"]
 FM_OPT_AUX_PLANAR, FM_OPT_SIDE_STREAMS, FM_OPT_LAZY_REG, FM_OPT_GRAPH, FM_OPT_DENSE_ROWS, FM_OPT_WIDE_ADDRESSES = range(6)
 
 _lib = None
@@ -72,10 +80,14 @@ def load() -> ctypes.CDLL:
                 "fm_evaluate": [vp] * 8, "fm_gradient": [vp] * 10, "fm_sgd_epoch": [vp] * 8,
                 "fm_minibatch_epoch": [vp] * 8, "fm_stratified_epoch": [vp] * 8, "fm_stratified_begin": [vp] * 7,
                 "fm_stratified_step": [vp, vp, i32] + [vp] * 5, "fm_stratified_end": [vp] * 4, "fm_get_aux": [vp] * 6,
-                "fm_profile_read": [vp] * 3, "fm_destroy": [vp]}.items():
+                "fm_profile_read": [vp] * 3, "fm_destroy": [vp],
+                "fm_field_create": [i64, i32, i64, i32, vp], "fm_field_destroy": [vp],
+                "fm_field_logprobs": [vp, vp, i64, vp, i64, i32] + [vp] * 4 + [i32] + [vp] * 3,
+                "fm_field_distill": [vp, vp, i64, vp, i64, i32] + [vp] * 8}.items():
             getattr(lib, name).argtypes = types
         _torch = torch
-        lib.fm_last_error.restype = ctypes.c_char_p
+        lib.fm_last_error.restype = lib.fm_field_last_error.restype = ctypes.c_char_p
+        lib.fm_field_last_error.argtypes = [ctypes.c_void_p]
         lib.fm_last_error.argtypes = [ctypes.c_void_p]
         lib.fm_profile_kernel_name.restype = ctypes.c_char_p
         _lib = lib
@@ -319,3 +331,105 @@ class Matrix:
         self._check(lib.fm_profile_read(self._h, _vp(launches), _vp(ms)))
         return {lib.fm_profile_kernel_name(ctypes.c_int32(k)).decode(): (int(launches[k]), float(ms[k]))
                 for k in range(nk)}
+
+
+def _rows(t, n, K, dtypes, what):
+    """Row stride of a CUDA tensor of n rows of K values, one after another in a row; a flat one is taken as contiguous."""
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype in dtypes):
+        raise TypeError(f"{what} must be a CUDA tensor of type {' or '.join(str(d) for d in dtypes)}")
+    if t.dim() == 1 and t.numel() == n * K and t.is_contiguous():
+        return K
+    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != K:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected ({n}, {K})")
+    if t.numel() and K > 1 and t.stride(1) != 1:
+        raise TypeError(f"the values of a row of {what} must be contiguous")
+    return max(K, t.stride(0)) if n <= 1 else t.stride(0)
+
+
+def _out(t, n, dtype, what):
+    if t is None:
+        return
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype is dtype and t.is_contiguous()):
+        raise TypeError(f"{what} must be a contiguous {dtype} CUDA tensor")
+    if t.numel() != n:
+        raise ValueError(f"{what} has {t.numel()} elements, expected {n}")
+
+
+class Field:
+    """Owner of an ``fm_field`` handle: the C candidates of a field with K latent values each, for calls of up to
+    ``max_rows`` rows that ask for up to ``max_top`` best candidates."""
+
+    def __init__(self, C, K, max_rows, max_top=0):
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU: the operators of a field only run on the HIP library")
+        lib = load()
+        self.C, self.K = int(C), int(K)
+        torch.cuda.current_stream()  # the runtime's device is torch's from here on
+        self._h = ctypes.c_void_p(None)
+        rc = lib.fm_field_create(self.C, self.K, int(max_rows), int(max_top), ctypes.byref(self._h))
+        if rc != FM_OK:
+            raise FMError(rc, (lib.fm_field_last_error(None) or b"").decode())
+
+    def _check(self, rc):
+        if rc != FM_OK:
+            raise FMError(rc, (load().fm_field_last_error(self._h) or b"").decode())
+
+    def close(self):
+        if self._h:
+            load().fm_field_destroy(self._h)
+            self._h = ctypes.c_void_p(None)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _candidates(self, n, V, w, mask, scale):
+        types = {_torch.float32: FM_TYPE_F32, _torch.float16: FM_TYPE_F16, _torch.bfloat16: FM_TYPE_BF16}
+        v_stride = _rows(V, self.C, self.K, tuple(types), "V")
+        _dev(w, self.C, "w")
+        mask_stride = 0
+        if mask is not None:
+            words = (self.C + 31) // 32
+            if not (isinstance(mask, _torch.Tensor) and mask.is_cuda and mask.dtype is _torch.int32):
+                raise TypeError("mask must be an int32 CUDA tensor, candidate j in bit j % 32 of word j // 32")
+            m = mask if mask.dim() == 2 else mask[None]
+            if m.dim() != 2 or m.shape[0] not in (1, n) or m.shape[1] != words:
+                raise ValueError(f"mask has shape {tuple(mask.shape)}, expected (1, {words}) or ({n}, {words})")
+            if words > 1 and m.numel() and m.stride(1) != 1:
+                raise TypeError("the words of a row's mask must be contiguous")
+            mask_stride = m.stride(0) if m.shape[0] > 1 else 0
+        return fm_candidates(V.data_ptr(), _vp(w), _vp(mask), v_stride, mask_stride, types[V.dtype], float(scale))
+
+    def fm_field_logprobs(self, G, V, w=None, mask=None, scale=1.0, ids=None, logprob=None, lse=None, entropy=None,
+                          top_ids=None, top_logprob=None, stream=None):
+        """G: rows x K float32; V: C x K float32, float16 or bfloat16; ids and logprob: rows x T; top_ids (int32) and
+        top_logprob: rows x top."""
+        n = G.shape[0] if G.dim() == 2 else G.numel() // self.K
+        g_stride = _rows(G, n, self.K, (_torch.float32,), "G")
+        c = self._candidates(n, V, w, mask, scale)
+        T = 0 if ids is None or n == 0 else ids.numel() // n
+        best = top_ids if top_ids is not None else top_logprob
+        top = 0 if best is None or n == 0 else best.numel() // n
+        f32, i32 = _torch.float32, _torch.int32
+        _out(ids, n * T, i32, "ids"); _out(logprob, n * T, f32, "logprob"); _out(lse, n, f32, "lse")
+        _out(entropy, n, f32, "entropy"); _out(top_ids, n * top, i32, "top_ids"); _out(top_logprob, n * top, f32, "top_logprob")
+        self._check(load().fm_field_logprobs(self._h, ctypes.byref(c), n, G.data_ptr(), g_stride, T, _vp(ids), _vp(logprob),
+                                             _vp(lse), _vp(entropy), top, _vp(top_ids), _vp(top_logprob), _stream(stream)))
+
+    def fm_field_distill(self, G, V, ids, teacher, w=None, mask=None, scale=1.0, weight=None, loss=None, grad_G=None,
+                         grad_V=None, grad_w=None, stream=None):
+        """ids (int32) and teacher: rows x T, the teacher's largest logits; weight: one value to a row."""
+        n = G.shape[0] if G.dim() == 2 else G.numel() // self.K
+        g_stride = _rows(G, n, self.K, (_torch.float32,), "G")
+        c = self._candidates(n, V, w, mask, scale)
+        T = 1 if n == 0 else ids.numel() // n
+        f32, K, C = _torch.float32, self.K, self.C
+        _out(ids, n * T, _torch.int32, "ids"); _out(teacher, n * T, f32, "teacher"); _out(weight, n, f32, "weight")
+        _out(loss, n, f32, "loss"); _out(grad_G, n * K, f32, "grad_G"); _out(grad_V, C * K, f32, "grad_V")
+        _out(grad_w, C, f32, "grad_w")
+        self._check(load().fm_field_distill(self._h, ctypes.byref(c), n, G.data_ptr(), g_stride, T, _vp(ids), _vp(teacher),
+                                            _vp(weight), _vp(loss), _vp(grad_G), _vp(grad_V), _vp(grad_w),
+                                            _stream(stream)))

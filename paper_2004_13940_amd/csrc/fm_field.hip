@@ -1,0 +1,520 @@
+// The candidates of a field: log probabilities, and distillation from a teacher's top logits.
+#include <math.h>
+#include <stdarg.h>
+#include <stdio.h>
+
+#include <new>
+
+#include "fm_field.h"
+
+namespace {
+
+// Order of logits as whole numbers: 0 for -infinity and NaN, which are never among the best.
+__device__ __forceinline__ uint32_t logit_key(float z)
+{
+    z += 0.f;  // one zero
+    if (!(z > -INFINITY)) return 0;
+    const uint32_t b = __float_as_uint(z);
+    return (int32_t)b < 0 ? ~b : b | 0x80000000u;
+}
+
+__device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k & 0x7FFFFFFFu : ~k); }
+
+template <int X>
+__device__ __forceinline__ uint64_t max_xor(uint64_t v)
+{
+    const uint32_t lo = (uint32_t)fm_xor_lane<X>((int)(uint32_t)v), hi = (uint32_t)fm_xor_lane<X>((int)(uint32_t)(v >> 32));
+    const uint64_t o = (uint64_t)hi << 32 | lo;
+    return o > v ? o : v;
+}
+
+__device__ __forceinline__ uint64_t wave_max(uint64_t v)
+{
+    return max_xor<1>(max_xor<2>(max_xor<4>(max_xor<8>(max_xor<16>(max_xor<32>(v))))));
+}
+
+// One wavefront per row and split.
+template <typename TV>
+__global__ __launch_bounds__(64) void k_field_stats(const FieldArgs A)
+{
+    __shared__ float g[256];
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    for (int k = lane; k < A.K; k += 64) g[k] = A.G[row * A.g_stride + k];
+    __syncthreads();
+    const int64_t beg = (int64_t)blockIdx.y * A.chunk, end = min(A.C, beg + A.chunk);
+    FieldPart p = {-INFINITY, 0.f, 0.f};
+    for (int64_t j0 = beg; j0 < end; j0 += FM_GROUP) {
+        const int64_t j = j0 + lane;
+        const float z = j < end ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
+        if (z != -INFINITY) p = fm_field_merge(p, {z * A.sl, z * A.sl < INFINITY ? 1.f : NAN, 0.f});
+        if (A.gmax != nullptr) {
+            float top = z;
+            for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+            if (lane == 0) A.gmax[row * A.ngroups + j0 / FM_GROUP] = top;
+        }
+    }
+    for (int x = 32; x > 0; x >>= 1)
+        p = fm_field_merge(p, {__shfl_xor(p.m, x), __shfl_xor(p.S, x), __shfl_xor(p.U, x)});
+    if (lane == 0) A.part[(int64_t)blockIdx.y * A.n + row] = make_float4(p.m, p.S, p.U, 0.f);
+}
+
+// Statistics of a row over all splits, the same in all threads of the workgroup.
+template <int BS>
+__device__ __forceinline__ FieldPart row_stats(const FieldArgs& A, int64_t row, FieldPart* lds)
+{
+    FieldPart p = {-INFINITY, 0.f, 0.f};
+    for (int s = threadIdx.x; s < A.splits; s += BS) {
+        const float4 q = A.part[(int64_t)s * A.n + row];
+        p = fm_field_merge(p, {q.x, q.y, q.z});
+    }
+    for (int x = 32; x > 0; x >>= 1)
+        p = fm_field_merge(p, {__shfl_xor(p.m, x), __shfl_xor(p.S, x), __shfl_xor(p.U, x)});
+    if constexpr (BS > 64) {
+        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = p;
+        __syncthreads();
+        p = lds[0];
+        for (int i = 1; i < BS / 64; ++i) p = fm_field_merge(p, lds[i]);
+    }
+    return p;
+}
+
+// Largest key below `below` that `key_at` gives for the items 0..count-1, keys being (order of the value, item counted from
+// the end), so that lower items come first among equal values.  0: none.  The same in all threads.
+template <int BS, typename F>
+__device__ __forceinline__ uint64_t next_best(int64_t count, uint64_t& mine, uint64_t below, uint64_t* lds, F key_at)
+{
+    if (mine >= below) {  // the thread's best was taken, or it has not looked yet
+        mine = 0;
+        for (int64_t i = threadIdx.x; i < count; i += BS) {
+            const uint64_t k = key_at(i);
+            if (k < below && k > mine) mine = k;
+        }
+    }
+    uint64_t best = wave_max(mine);
+    if constexpr (BS > 64) {
+        __syncthreads();
+        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = best;
+        __syncthreads();
+        best = lds[0];
+        for (int i = 1; i < BS / 64; ++i) best = lds[i] > best ? lds[i] : best;
+    }
+    return best;
+}
+
+__device__ __forceinline__ uint64_t item_key(float z, int64_t i)
+{
+    const uint32_t k = logit_key(z);
+    return k == 0 ? 0 : (uint64_t)k << 32 | (uint32_t)~(uint32_t)i;
+}
+
+// What is left of a row: its sums joined, given candidates, best candidates.
+template <typename TV, int BS>
+__global__ __launch_bounds__(BS) void k_field_finish(const FieldArgs A)
+{
+    __shared__ float g[256];
+    __shared__ FieldPart parts[BS / 64];
+    __shared__ uint64_t best[BS / 64];
+    __shared__ int32_t groups[FM_FIELD_TOP];
+    __shared__ float zs[FM_FIELD_TOP * FM_GROUP];
+    const int64_t row = blockIdx.x;
+    for (int k = threadIdx.x; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
+    const FieldPart p = row_stats<BS>(A, row, parts);
+    __syncthreads();
+    const bool empty = p.S == 0.f;
+    const float log2S = __builtin_amdgcn_logf(p.S);
+    if (threadIdx.x == 0) {
+        if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
+        if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
+    }
+    const auto logprob = [&](float z) {
+        return p.S != p.S ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
+    };
+    if (A.logprob != nullptr)
+        for (int t = threadIdx.x; t < A.T; t += BS) {
+            const int64_t j = A.ids[row * A.T + t];
+            A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
+        }
+    if (A.gmax == nullptr) return;
+    // candidates: groups of groups, of these the groups, of these the candidates
+    const float* gm = A.gmax + row * A.ngroups;
+    const bool nan = p.S != p.S;
+    uint64_t mine = ~0ull, below = ~0ull;
+    int nsel = 0;
+    const int64_t nsuper = (A.ngroups + FM_GROUPS - 1) / FM_GROUPS;
+    for (; !nan && nsel < A.top; ++nsel) {
+        below = next_best<BS>(nsuper, mine, below, best, [&](int64_t i) {
+            float z = -INFINITY;
+            for (int64_t q = i * FM_GROUPS; q < min(A.ngroups, (i + 1) * FM_GROUPS); ++q) z = fmaxf(z, gm[q]);
+            return item_key(z, i);
+        });
+        if (below == 0) break;
+        if (threadIdx.x == 0) groups[nsel] = (int32_t)~(uint32_t)below;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < nsel * FM_GROUPS; i += BS) {
+        const int64_t q = (int64_t)groups[i / FM_GROUPS] * FM_GROUPS + i % FM_GROUPS;
+        zs[i] = q < A.ngroups ? gm[q] : -INFINITY;
+    }
+    __syncthreads();
+    const int nq = nsel * FM_GROUPS;
+    // the groups taken are in the order of their maxima, not of their numbers: keys are made of the numbers
+    mine = below = ~0ull;
+    nsel = 0;
+    int32_t taken = 0;  // of thread a: the a-th group taken
+    for (; !nan && nsel < A.top; ++nsel) {
+        below = next_best<BS>(nq, mine, below, best, [&](int64_t i) {
+            return item_key(zs[i], (int64_t)groups[i / FM_GROUPS] * FM_GROUPS + i % FM_GROUPS);
+        });
+        if (below == 0) break;
+        if (threadIdx.x == nsel) taken = (int32_t)~(uint32_t)below;
+    }
+    __syncthreads();
+    if ((int)threadIdx.x < nsel) groups[threadIdx.x] = taken;
+    __syncthreads();
+    for (int i = threadIdx.x; i < nsel * FM_GROUP; i += BS) {
+        const int64_t j = (int64_t)groups[i / FM_GROUP] * FM_GROUP + i % FM_GROUP;
+        zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
+    }
+    __syncthreads();
+    const int nj = nsel * FM_GROUP;
+    mine = below = ~0ull;
+    for (int a = 0; a < A.top; ++a) {
+        if (below != 0 && nj > 0)
+            below = next_best<BS>(nj, mine, below, best, [&](int64_t i) {
+                return item_key(zs[i], (int64_t)groups[i / FM_GROUP] * FM_GROUP + i % FM_GROUP);
+            });
+        else
+            below = 0;
+        if (threadIdx.x == 0) {
+            const bool none = below == 0;
+            if (A.top_ids != nullptr) A.top_ids[row * A.top + a] = none ? -1 : (int32_t)~(uint32_t)below;
+            if (A.top_logprob != nullptr)
+                A.top_logprob[row * A.top + a] = nan ? NAN : none ? -INFINITY : logprob(key_logit((uint32_t)(below >> 32)));
+        }
+    }
+}
+
+// Row i: loss, its gradient by G, and what the columns need of it.  One wavefront to a row.
+template <typename TV>
+__global__ __launch_bounds__(64) void k_field_distill_rows(const FieldArgs A)
+{
+    __shared__ float g[256];
+    __shared__ float ps[64];
+    const int lane = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    for (int k = lane; k < A.K; k += 64) g[k] = A.G[row * A.g_stride + k];
+    __syncthreads();
+    const FieldPart p = row_stats<64>(A, row, nullptr);
+    const float log2S = __builtin_amdgcn_logf(p.S);
+    // the teacher's softmax over its entries that the row allows
+    const TV* V = static_cast<const TV*>(A.V);
+    float mt = -INFINITY, Q = 0.f;
+    for (int pass = 0; pass < 2; ++pass) {
+        float x = pass == 0 ? -INFINITY : 0.f;
+        for (int t = lane; t < A.T; t += 64) {
+            const int64_t j = A.ids[row * A.T + t];
+            if (j < 0 || j >= A.C || fm_field_logit<TV>(A, row, g, j) == -INFINITY) continue;
+            const float y = A.teacher[row * A.T + t] * A.sl;
+            x = pass == 0 ? fmaxf(x, y) : x + __builtin_amdgcn_exp2f(y - mt);
+        }
+        for (int d = 32; d > 0; d >>= 1) {
+            const float o = __shfl_xor(x, d);
+            x = pass == 0 ? fmaxf(x, o) : x + o;
+        }
+        (pass == 0 ? mt : Q) = x;
+    }
+    const bool takes = Q != 0.f;  // Q is 0 without entries
+    const float log2Q = __builtin_amdgcn_logf(Q), r = takes ? (A.weight != nullptr ? A.weight[row] : 1.f) * A.scale : 0.f;
+    float loss = 0.f;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    if (takes) {
+        for (int t0 = 0; t0 < A.T; t0 += 64) {
+            const int t = t0 + lane;
+            const int64_t j = t < A.T ? A.ids[row * A.T + t] : -1;
+            float q = 0.f;
+            if (j >= 0 && j < A.C) {
+                const float z = fm_field_logit<TV>(A, row, g, j);
+                if (z != -INFINITY) {
+                    const float y = A.teacher[row * A.T + t] * A.sl - mt;
+                    q = __builtin_amdgcn_exp2f(y) / Q;
+                    const float d = (y - log2Q) - (fmaf(z, A.sl, -p.m) - log2S);
+                    loss += q == 0.f ? 0.f : q * d * FM_LN2;
+                }
+            }
+            if (r == 0.f) continue;
+            for (int l = 0; l < 64; ++l) {
+                const float d = __shfl(q, l);
+                const int64_t jl = __shfl((int)j, l);
+                if (d != 0.f)
+                    for (int c = 0; c < 4; ++c)
+                        if (lane + 64 * c < A.K) acc[c] -= r * d * fm_field_value(V + jl * A.v_stride + lane + 64 * c);
+            }
+        }
+        for (int d = 32; d > 0; d >>= 1) loss += __shfl_xor(loss, d);
+    }
+    if (lane == 0) {
+        if (A.loss != nullptr) A.loss[row] = loss;
+        A.rows[row] = make_float4(p.m, r == 0.f ? 0.f : r / p.S, mt, takes ? r / Q : 0.f);
+    }
+    if (A.grad_G == nullptr) return;
+    if (r != 0.f)
+        for (int64_t j0 = 0; j0 < A.C; j0 += 64) {
+            const int64_t j = j0 + lane;
+            const float z = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
+            ps[lane] = z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(z, A.sl, -p.m)) * (r / p.S);
+            __syncthreads();
+            for (int l = 0; l < 64; ++l) {
+                const float d = ps[l];
+                if (d != 0.f)
+                    for (int c = 0; c < 4; ++c)
+                        if (lane + 64 * c < A.K) acc[c] += d * fm_field_value(V + (j0 + l) * A.v_stride + lane + 64 * c);
+            }
+            __syncthreads();
+        }
+    for (int c = 0; c < 4; ++c)
+        if (lane + 64 * c < A.K) A.grad_G[row * A.K + lane + 64 * c] = acc[c];
+}
+
+// Candidate j: its gradient.  One wavefront to a candidate.
+template <typename TV>
+__global__ __launch_bounds__(64) void k_field_distill_cols(const FieldArgs A)
+{
+    const int lane = threadIdx.x;
+    const int64_t j = blockIdx.x;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, gw = 0.f;
+    for (int64_t i0 = 0; i0 < A.n; i0 += 64) {
+        const int64_t row = i0 + lane;
+        float d = 0.f;
+        if (row < A.n) {
+            const float4 info = A.rows[row];
+            if (info.y != 0.f) {
+                const float z = fm_field_logit<TV>(A, row, A.G + row * A.g_stride, j);
+                if (z != -INFINITY) {
+                    d = __builtin_amdgcn_exp2f(fmaf(z, A.sl, -info.x)) * info.y;
+                    for (int t = 0; t < A.T; ++t)
+                        if (A.ids[row * A.T + t] == j)
+                            d -= __builtin_amdgcn_exp2f(A.teacher[row * A.T + t] * A.sl - info.z) * info.w;
+                }
+            }
+        }
+        gw += d;
+        for (int l = 0; l < 64; ++l) {
+            const float dl = __shfl(d, l);
+            if (dl != 0.f)
+                for (int c = 0; c < 4; ++c)
+                    if (lane + 64 * c < A.K) acc[c] += dl * A.G[(i0 + l) * A.g_stride + lane + 64 * c];
+        }
+    }
+    for (int x = 32; x > 0; x >>= 1) gw += __shfl_xor(gw, x);
+    if (A.grad_w != nullptr && lane == 0) A.grad_w[j] = gw;
+    if (A.grad_V != nullptr)
+        for (int c = 0; c < 4; ++c)
+            if (lane + 64 * c < A.K) A.grad_V[j * A.K + lane + 64 * c] = acc[c];
+}
+
+constexpr int FIELD_SLOTS = 4096;                     // wavefronts that the rows of a small call are split into
+constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
+
+}  // namespace
+
+struct fm_field {
+    int64_t C, max_rows;
+    int32_t K, max_top;
+    int device;
+    char* block;      // the workspace
+    int64_t slots;    // FieldParts in it
+    int64_t top_rows; // rows whose group maxima fit
+    char err[256];
+};
+
+namespace {
+
+thread_local char g_create_error[256];
+
+int fail(fm_field* f, int code, const char* fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(f != nullptr ? f->err : g_create_error, sizeof(g_create_error), fmt, ap);
+    va_end(ap);
+    return code;
+}
+
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+size_t room(int64_t bytes) { return (size_t)up(bytes, 256) * 256; }
+
+int32_t splits_of(const fm_field* f, int64_t n)
+{
+    return (int32_t)std::max<int64_t>(1, std::min(up(FIELD_SLOTS, n), up(f->C, FM_GROUP)));
+}
+
+int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
+{
+    if (c == nullptr || c->V == nullptr) return fail(f, FM_EINVAL, "candidates and their V must not be NULL");
+    if (n < 0 || n > f->max_rows) return fail(f, FM_ERANGE, "n=%lld outside 0..%lld", (long long)n, (long long)f->max_rows);
+    if (n > 0 && G == nullptr) return fail(f, FM_EINVAL, "G must not be NULL");
+    if (c->v_type < FM_TYPE_F32 || c->v_type > FM_TYPE_BF16) return fail(f, FM_EINVAL, "unknown type %d of V", c->v_type);
+    if (!(c->scale > 0.f) || !(c->scale < INFINITY)) return fail(f, FM_EINVAL, "scale must be positive and finite");
+    const int64_t most = int64_t(1) << 40;
+    if (c->v_stride < f->K || c->v_stride > most || (n > 1 && (g_stride < f->K || g_stride > most)))
+        return fail(f, FM_EINVAL, "strides of V (%lld) and G (%lld) must be at least K=%d", (long long)c->v_stride, (long long)g_stride, f->K);
+    if (c->mask != nullptr && c->mask_stride != 0 && (c->mask_stride < up(f->C, 32) || c->mask_stride > most))
+        return fail(f, FM_EINVAL, "mask_stride=%lld: 0, or at least %lld words", (long long)c->mask_stride, (long long)up(f->C, 32));
+    const uintptr_t size = c->v_type == FM_TYPE_F32 ? 4 : 2;
+    if ((uintptr_t)c->V % size != 0 || (uintptr_t)c->w % 4 != 0 || (uintptr_t)c->mask % 4 != 0 || (uintptr_t)G % 4 != 0)
+        return fail(f, FM_EINVAL, "V, w, mask and G must be aligned like their values");
+    int dev = -1;
+    if (hipGetDevice(&dev) != hipSuccess || dev != f->device)
+        return fail(f, FM_ESTATE, "the handle was created on device %d, the current one is %d", f->device, dev);
+    return FM_OK;
+}
+
+FieldArgs arguments(const fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
+{
+    FieldArgs A = {};
+    A.V = c->V;
+    A.w = c->w;
+    A.mask = c->mask;
+    A.v_stride = c->v_stride;
+    A.mask_stride = c->mask_stride;
+    A.G = G;
+    A.g_stride = g_stride;
+    A.C = f->C;
+    A.K = f->K;
+    A.n = (int32_t)n;
+    A.scale = c->scale;
+    A.sl = c->scale * FM_LOG2E;
+    A.splits = splits_of(f, n);
+    A.chunk = up(up(f->C, A.splits), FM_GROUP) * FM_GROUP;
+    A.splits = (int32_t)up(f->C, A.chunk);
+    A.part = reinterpret_cast<float4*>(f->block);
+    A.rows = reinterpret_cast<float4*>(f->block + room(f->slots * 16));
+    A.ngroups = up(f->C, FM_GROUP);
+    return A;
+}
+
+int launched(fm_field* f)
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? FM_OK : fail(f, FM_EHIP, "launch failed: %s", hipGetErrorString(e));
+}
+
+template <typename F>
+int by_type(int32_t type, F run)
+{
+    switch (type) {
+        case FM_TYPE_F16: return run((_Float16*)nullptr);
+        case FM_TYPE_BF16: return run((__bf16*)nullptr);
+        default: return run((float*)nullptr);
+    }
+}
+
+}  // namespace
+
+extern "C" const char* fm_field_last_error(const fm_field* f) { return f != nullptr ? f->err : g_create_error; }
+
+extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t max_top, fm_field** out)
+{
+    if (out == nullptr) return fail(nullptr, FM_EINVAL, "out must not be NULL");
+    *out = nullptr;
+    int vec, lanes;
+    if (!fm_shape_for_K(K, &vec, &lanes)) return fail(nullptr, FM_EINVAL, "K=%d unsupported (1..64, or a multiple of 4 up to 256)", K);
+    if (C < 1 || C > INT32_MAX || max_rows < 1 || max_rows > INT32_MAX)
+        return fail(nullptr, FM_ERANGE, "C=%lld and max_rows=%lld must be 1..2^31-1", (long long)C, (long long)max_rows);
+    if (max_top < 0 || max_top > FM_FIELD_TOP) return fail(nullptr, FM_ERANGE, "max_top=%d outside 0..%d", max_top, FM_FIELD_TOP);
+    fm_field* f = new (std::nothrow) fm_field();
+    if (f == nullptr) return fail(nullptr, FM_ENOMEM, "no host memory");
+    f->C = C;
+    f->K = K;
+    f->max_rows = max_rows;
+    f->max_top = max_top;
+    f->slots = max_rows + FIELD_SLOTS;
+    f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / up(C, FM_GROUP)));
+    const size_t bytes = room(f->slots * 16) + room(max_rows * 16) + room(f->top_rows * up(C, FM_GROUP) * 4);
+    hipError_t e = hipGetDevice(&f->device);
+    if (e == hipSuccess) e = hipMalloc((void**)&f->block, bytes);
+    if (e != hipSuccess) {  // what closed handles left may be what is missing
+        (void)hipGetLastError();
+        fm_trim();
+        e = hipMalloc((void**)&f->block, bytes);
+    }
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        delete f;
+        return fail(nullptr, FM_ENOMEM, "hipMalloc of %zu bytes failed: %s", bytes, hipGetErrorString(e));
+    }
+    *out = f;
+    return FM_OK;
+}
+
+extern "C" int fm_field_destroy(fm_field* f)
+{
+    if (f == nullptr) return FM_OK;
+    (void)hipFree(f->block);
+    delete f;
+    return FM_OK;
+}
+
+extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride, int32_t T,
+                                 const int32_t* ids, float* logprob, float* lse, float* entropy, int32_t top,
+                                 int32_t* top_ids, float* top_logprob, void* hip_stream)
+{
+    if (f == nullptr) return FM_EINVAL;
+    FM_TRY(check(f, c, n, G, g_stride));
+    if (T < 0 || (logprob != nullptr && T > 0 && ids == nullptr)) return fail(f, FM_EINVAL, "logprob needs ids, and T=%d >= 0", T);
+    if (top < 0 || top > f->max_top) return fail(f, FM_ERANGE, "top=%d outside 0..%d", top, f->max_top);
+    if (n == 0) return FM_OK;
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (top_ids == nullptr && top_logprob == nullptr) top = 0;
+    const int64_t step = top > 0 ? f->top_rows : n;
+    for (int64_t at = 0; at < n; at += step) {
+        FieldArgs A = arguments(f, c, std::min(step, n - at), G + at * g_stride, g_stride);
+        if (A.mask != nullptr) A.mask += at * A.mask_stride;
+        A.T = T;
+        A.top = top;
+        A.ids = ids != nullptr ? ids + at * T : nullptr;
+        A.logprob = logprob != nullptr && T > 0 ? logprob + at * T : nullptr;
+        A.lse = lse != nullptr ? lse + at : nullptr;
+        A.entropy = entropy != nullptr ? entropy + at : nullptr;
+        A.top_ids = top_ids != nullptr ? top_ids + at * top : nullptr;
+        A.top_logprob = top_logprob != nullptr ? top_logprob + at * top : nullptr;
+        A.gmax = top > 0 ? reinterpret_cast<float*>(f->block + room(f->slots * 16) + room(f->max_rows * 16)) : nullptr;
+        FM_TRY(by_type(c->v_type, [&](auto* t) {
+            using TV = std::remove_pointer_t<decltype(t)>;
+            k_field_stats<TV><<<dim3((uint32_t)A.n, (uint32_t)A.splits), 64, 0, st>>>(A);
+            k_field_finish<TV, FM_BLOCK><<<(uint32_t)A.n, FM_BLOCK, 0, st>>>(A);
+            return launched(f);
+        }));
+    }
+    return FM_OK;
+}
+
+extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride, int32_t T,
+                                const int32_t* ids, const float* teacher, const float* weight, float* loss, float* grad_G,
+                                float* grad_V, float* grad_w, void* hip_stream)
+{
+    if (f == nullptr) return FM_EINVAL;
+    FM_TRY(check(f, c, n, G, g_stride));
+    if (T < 1 || (n > 0 && (ids == nullptr || teacher == nullptr))) return fail(f, FM_EINVAL, "ids and teacher of T=%d >= 1 entries to a row are needed", T);
+    hipStream_t st = (hipStream_t)hip_stream;
+    FieldArgs A = arguments(f, c, std::max<int64_t>(n, 1), G, g_stride);
+    A.n = (int32_t)n;
+    A.T = T;
+    A.ids = ids;
+    A.teacher = teacher;
+    A.weight = weight;
+    A.loss = loss;
+    A.grad_G = grad_G;
+    A.grad_V = grad_V;
+    A.grad_w = grad_w;
+    return by_type(c->v_type, [&](auto* t) {
+        using TV = std::remove_pointer_t<decltype(t)>;
+        if (n > 0) {
+            k_field_stats<TV><<<dim3((uint32_t)n, (uint32_t)A.splits), 64, 0, st>>>(A);
+            k_field_distill_rows<TV><<<(uint32_t)n, 64, 0, st>>>(A);
+        }
+        if (grad_V != nullptr || grad_w != nullptr) k_field_distill_cols<TV><<<(uint32_t)A.C, 64, 0, st>>>(A);
+        return launched(f);
+    });
+}

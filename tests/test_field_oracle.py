@@ -1,0 +1,88 @@
+"""The oracle of the operators over the candidates of a field: against brute force, differences and the factorization
+machine's own score."""
+import numpy as np
+import pytest
+
+from oracle import field_oracle as F
+from oracle import fm_oracle as O
+
+
+def _case(seed, n=5, C=17, K=3, T=4):
+    rng = np.random.default_rng(seed)
+    ids = np.stack([rng.permutation(C)[:T] for _ in range(n)])
+    return rng, rng.normal(size=(n, K)), rng.normal(size=(C, K)), rng.normal(size=C), ids, rng.normal(size=(n, T))
+
+
+def test_logits_are_the_change_of_the_score_by_a_candidate():
+    """FM score of a row with candidate j's column set to 1, less that of the row without it."""
+    rng = np.random.default_rng(3)
+    N, D, C, K = 4, 12, 5, 3  # the last C columns are the field
+    X = np.zeros((N, D))
+    X[:, :D - C] = rng.normal(size=(N, D - C))
+    w, V = rng.normal(size=D), rng.normal(size=(D, K))
+
+    def score(X):
+        rowptr = np.concatenate([[0], np.cumsum((X != 0).sum(1))]).astype(np.int64)
+        col = np.nonzero(X)[1].astype(np.int32)
+        M = O.make_matrix(N, D, rowptr, col, X[X != 0])
+        a, G, q, yh = O.forward(M, 0.3, w, V)
+        return np.asarray(G).reshape(N, K), np.asarray(yh)
+
+    G, base = score(X)
+    z = F.logits(G, V[D - C:], w[D - C:])
+    for j in range(C):
+        Y = X.copy()
+        Y[:, D - C + j] = 1.0
+        np.testing.assert_allclose(score(Y)[1] - base, z[:, j], rtol=0, atol=1e-6)  # the oracle takes fp32 values
+
+
+def test_probabilities_entropy_and_best():
+    _, G, V, w, ids, _ = _case(1)
+    z = F.logits(G, V, w)
+    out = F.logprobs(z, 0.7, ids, top=3)
+    p = np.exp(0.7 * z) / np.exp(0.7 * z).sum(1, keepdims=True)
+    np.testing.assert_allclose(out["logprob"], np.log(np.take_along_axis(p, ids, 1)), rtol=1e-12)
+    np.testing.assert_allclose(out["entropy"], -(p * np.log(p)).sum(1), rtol=1e-12)
+    np.testing.assert_array_equal(out["top_ids"], np.argsort(-z, 1, kind="stable")[:, :3])
+    z[0, :] = -np.inf
+    out = F.logprobs(z, 1.0, ids, top=3)
+    assert out["lse"][0] == -np.inf and out["entropy"][0] == 0 and (out["top_ids"][0] == -1).all()
+
+
+@pytest.mark.parametrize("weighted", [False, True])
+def test_gradients_are_the_differences_of_the_loss(weighted):
+    rng, G, V, w, ids, teacher = _case(2)
+    ids[1, 2] = -1
+    ids[2, :] = -1  # a row without entries
+    allowed = rng.random((5, 17)) < 0.8
+    allowed[3] = False
+    allowed[0, ids[0, 0]] = False  # an entry that the row does not allow
+    weight = rng.random(5) if weighted else None
+
+    def total(G, V, w):
+        r = F.distill(F.logits(G, V, w, allowed), G, V, 0.6, ids, teacher, weight)
+        return r, float((r["loss"] * (1.0 if weight is None else weight)).sum())
+
+    out, _ = total(G, V, w)
+    assert out["loss"][2] == out["loss"][3] == 0 and (out["loss"][[0, 1, 4]] > 0).all()
+    h = 1e-6
+    for name, x in (("grad_G", G), ("grad_V", V), ("grad_w", w)):
+        for at in np.ndindex(x.shape):
+            keep = x[at]
+            x[at] = keep + h
+            up = total(G, V, w)[1]
+            x[at] = keep - h
+            down = total(G, V, w)[1]
+            x[at] = keep
+            assert abs((up - down) / (2 * h) - out[name][at]) < 1e-7, (name, at)
+
+
+def test_what_is_left_out_may_hold_anything():
+    _, G, V, w, ids, teacher = _case(4)
+    allowed = np.ones(17, bool)
+    allowed[[2, 9]] = False
+    clean = F.distill(F.logits(G, V, w, allowed), G, V, 1.0, ids, teacher)
+    V[2], w[9] = np.nan, np.inf
+    dirty = F.distill(F.logits(G, V, w, allowed), G, V, 1.0, ids, teacher)
+    for k in clean:
+        np.testing.assert_array_equal(clean[k], dirty[k])
