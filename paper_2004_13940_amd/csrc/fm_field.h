@@ -42,10 +42,11 @@ struct FieldArgs {
     int64_t C;
     int32_t n, K;
     float scale, sl;  // sl = scale log2(e)
-    // workspace
-    float4* part;     // [splits][n] FieldPart
-    int32_t splits;
+    // rows against parts of the candidates
+    int32_t row_tiles, splits;
     int64_t chunk;    // candidates to a split, a multiple of FM_GROUP
+    float4* part;     // [splits][n] FieldPart
+    float* opart;     // [splits][n][KP] sum 2^(x - m) v_j (distillation)
     float* gmax;      // [n][ngroups] largest logit of every group, or nullptr
     int64_t ngroups;
     // logprobs
@@ -56,7 +57,17 @@ struct FieldArgs {
     // distillation
     const float *teacher, *weight;
     float *loss, *grad_G, *grad_V, *grad_w;
-    float4* rows;     // [n] reference m, weight scale / S (0: no part in the gradient), largest scaled teacher logit, weight scale / Q
+    int32_t npad;     // n in whole tiles of 16 rows
+    float* rm;        // [npad] reference m of the row's exponentials
+    float* rs;        // [npad] weight scale / S; 0: no part in the gradient
+    float2* rq;       // [npad] largest scaled teacher logit; S / Q, the share of the teacher in units of the exponentials
+    float* g0;        // [npad][KP] G, 0 for rows without a part in the gradient, NaN for rows that are NaN
+    float* gs;        // [npad][KP] rs G, finite
+    uint32_t* hits;   // [npad / 16][hit_words] blocks of 2^hit_shift candidates that some row of the tile names
+    int32_t hit_words, hit_shift;
+    int32_t col_tiles, row_splits, row_chunk;  // candidates against parts of the rows, multiples of 16 rows
+    float* vpart;     // [row_splits][C][KP] parts of grad_V, and [row_splits][C] of grad_w
+    float* wpart;
 };
 
 __device__ __forceinline__ float fm_field_value(const float* p) { return *p; }

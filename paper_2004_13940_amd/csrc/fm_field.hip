@@ -5,7 +5,7 @@
 
 #include <new>
 
-#include "fm_field.h"
+#include "fm_field_tiles.h"
 
 namespace {
 
@@ -31,32 +31,6 @@ __device__ __forceinline__ uint64_t max_xor(uint64_t v)
 __device__ __forceinline__ uint64_t wave_max(uint64_t v)
 {
     return max_xor<1>(max_xor<2>(max_xor<4>(max_xor<8>(max_xor<16>(max_xor<32>(v))))));
-}
-
-// One wavefront per row and split.
-template <typename TV>
-__global__ __launch_bounds__(64) void k_field_stats(const FieldArgs A)
-{
-    __shared__ float g[256];
-    const int lane = threadIdx.x;
-    const int64_t row = blockIdx.x;
-    for (int k = lane; k < A.K; k += 64) g[k] = A.G[row * A.g_stride + k];
-    __syncthreads();
-    const int64_t beg = (int64_t)blockIdx.y * A.chunk, end = min(A.C, beg + A.chunk);
-    FieldPart p = {-INFINITY, 0.f, 0.f};
-    for (int64_t j0 = beg; j0 < end; j0 += FM_GROUP) {
-        const int64_t j = j0 + lane;
-        const float z = j < end ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
-        if (z != -INFINITY) p = fm_field_merge(p, {z * A.sl, z * A.sl < INFINITY ? 1.f : NAN, 0.f});
-        if (A.gmax != nullptr) {
-            float top = z;
-            for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
-            if (lane == 0) A.gmax[row * A.ngroups + j0 / FM_GROUP] = top;
-        }
-    }
-    for (int x = 32; x > 0; x >>= 1)
-        p = fm_field_merge(p, {__shfl_xor(p.m, x), __shfl_xor(p.S, x), __shfl_xor(p.U, x)});
-    if (lane == 0) A.part[(int64_t)blockIdx.y * A.n + row] = make_float4(p.m, p.S, p.U, 0.f);
 }
 
 // Statistics of a row over all splits, the same in all threads of the workgroup.
@@ -195,126 +169,117 @@ __global__ __launch_bounds__(BS) void k_field_finish(const FieldArgs A)
     }
 }
 
-// Row i: loss, its gradient by G, and what the columns need of it.  One wavefront to a row.
-template <typename TV>
-__global__ __launch_bounds__(64) void k_field_distill_rows(const FieldArgs A)
+// Row i: loss, its gradient by G, and what the candidates need of it.  Rows beyond n, up to a whole tile, are empty ones.
+template <typename TV, int BS>
+__global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A, int32_t KP)
 {
     __shared__ float g[256];
-    __shared__ float ps[64];
-    const int lane = threadIdx.x;
+    __shared__ FieldPart parts[BS / 64];
+    __shared__ float sums[BS / 64], wide[BS];
+    const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
-    for (int k = lane; k < A.K; k += 64) g[k] = A.G[row * A.g_stride + k];
+    if (row >= A.n) {
+        for (int k = tid; k < KP; k += BS) A.g0[row * KP + k] = A.gs[row * KP + k] = 0.f;
+        if (tid == 0) A.rm[row] = 3e38f, A.rs[row] = 0.f, A.rq[row] = make_float2(0.f, 0.f);
+        return;
+    }
+    for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
+    const FieldPart p = row_stats<BS>(A, row, parts);
     __syncthreads();
-    const FieldPart p = row_stats<64>(A, row, nullptr);
     const float log2S = __builtin_amdgcn_logf(p.S);
-    // the teacher's softmax over its entries that the row allows
-    const TV* V = static_cast<const TV*>(A.V);
-    float mt = -INFINITY, Q = 0.f;
-    for (int pass = 0; pass < 2; ++pass) {
-        float x = pass == 0 ? -INFINITY : 0.f;
-        for (int t = lane; t < A.T; t += 64) {
-            const int64_t j = A.ids[row * A.T + t];
-            if (j < 0 || j >= A.C || fm_field_logit<TV>(A, row, g, j) == -INFINITY) continue;
-            const float y = A.teacher[row * A.T + t] * A.sl;
-            x = pass == 0 ? fmaxf(x, y) : x + __builtin_amdgcn_exp2f(y - mt);
-        }
+    const auto block = [&](float x, bool largest) {
         for (int d = 32; d > 0; d >>= 1) {
             const float o = __shfl_xor(x, d);
-            x = pass == 0 ? fmaxf(x, o) : x + o;
+            x = largest ? fmaxf(x, o) : x + o;
         }
-        (pass == 0 ? mt : Q) = x;
-    }
-    const bool takes = Q != 0.f;  // Q is 0 without entries
+        if constexpr (BS > 64) {
+            __syncthreads();
+            if (tid % 64 == 0) sums[tid / 64] = x;
+            __syncthreads();
+            x = sums[0];
+            for (int i = 1; i < BS / 64; ++i) x = largest ? fmaxf(x, sums[i]) : x + sums[i];
+        }
+        return x;
+    };
+    // the teacher's softmax over its entries that the row allows
+    const TV* V = static_cast<const TV*>(A.V);
+    const int32_t* ids = A.ids + row * A.T;
+    const float* teacher = A.teacher + row * A.T;
+    const auto entry = [&](int t, float& z) {
+        const int64_t j = ids[t];
+        if (j < 0 || j >= A.C) return false;
+        z = fm_field_logit<TV>(A, row, g, j);
+        return z != -INFINITY && teacher[t] != -INFINITY;
+    };
+    float x = -INFINITY, z;
+    for (int t = tid; t < A.T; t += BS)
+        if (entry(t, z)) x = fmaxf(x, teacher[t] * A.sl);
+    const float mt = block(x, true);
+    x = 0.f;
+    for (int t = tid; t < A.T; t += BS)
+        if (entry(t, z)) x += __builtin_amdgcn_exp2f(teacher[t] * A.sl - mt);
+    const float Q = block(x, false);
+    const bool takes = Q != 0.f, nan = p.S != p.S;
     const float log2Q = __builtin_amdgcn_logf(Q), r = takes ? (A.weight != nullptr ? A.weight[row] : 1.f) * A.scale : 0.f;
-    float loss = 0.f;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    if (takes) {
-        for (int t0 = 0; t0 < A.T; t0 += 64) {
-            const int t = t0 + lane;
-            const int64_t j = t < A.T ? A.ids[row * A.T + t] : -1;
-            float q = 0.f;
-            if (j >= 0 && j < A.C) {
-                const float z = fm_field_logit<TV>(A, row, g, j);
-                if (z != -INFINITY) {
-                    const float y = A.teacher[row * A.T + t] * A.sl - mt;
-                    q = __builtin_amdgcn_exp2f(y) / Q;
-                    const float d = (y - log2Q) - (fmaf(z, A.sl, -p.m) - log2S);
-                    loss += q == 0.f ? 0.f : q * d * FM_LN2;
+    const bool counts = r != 0.f;
+    x = 0.f;
+    if (takes)
+        for (int t = tid; t < A.T; t += BS)
+            if (entry(t, z)) {
+                const float y = teacher[t] * A.sl - mt, q = __builtin_amdgcn_exp2f(y) / Q;
+                const float d = (y - log2Q) - (fmaf(z, A.sl, -p.m) - log2S);
+                if (q != 0.f) x += q * d * FM_LN2;
+                if (counts) {
+                    const int64_t block = ids[t] >> A.hit_shift;
+                    atomicOr(A.hits + row / 16 * A.hit_words + (block >> 5), 1u << (block & 31));
                 }
             }
-            if (r == 0.f) continue;
-            for (int l = 0; l < 64; ++l) {
-                const float d = __shfl(q, l);
-                const int64_t jl = __shfl((int)j, l);
-                if (d != 0.f)
-                    for (int c = 0; c < 4; ++c)
-                        if (lane + 64 * c < A.K) acc[c] -= r * d * fm_field_value(V + jl * A.v_stride + lane + 64 * c);
-            }
-        }
-        for (int d = 32; d > 0; d >>= 1) loss += __shfl_xor(loss, d);
+    x = block(x, false);
+    const float rs = counts ? r / p.S : 0.f;
+    if (tid == 0) {
+        if (A.loss != nullptr) A.loss[row] = x;
+        A.rm[row] = !counts ? 3e38f : nan ? 0.f : p.m;
+        A.rs[row] = nan ? 0.f : rs;
+        A.rq[row] = make_float2(mt, counts && !nan ? p.S / Q : 0.f);
     }
-    if (lane == 0) {
-        if (A.loss != nullptr) A.loss[row] = loss;
-        A.rows[row] = make_float4(p.m, r == 0.f ? 0.f : r / p.S, mt, takes ? r / Q : 0.f);
+    for (int k = tid; k < KP; k += BS) {
+        const float v = k < A.K ? g[k] : 0.f;
+        A.g0[row * KP + k] = !counts ? 0.f : nan ? NAN : v;
+        A.gs[row * KP + k] = !counts || nan ? 0.f : rs * v;
     }
     if (A.grad_G == nullptr) return;
-    if (r != 0.f)
-        for (int64_t j0 = 0; j0 < A.C; j0 += 64) {
-            const int64_t j = j0 + lane;
-            const float z = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
-            ps[lane] = z == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(z, A.sl, -p.m)) * (r / p.S);
-            __syncthreads();
-            for (int l = 0; l < 64; ++l) {
-                const float d = ps[l];
-                if (d != 0.f)
-                    for (int c = 0; c < 4; ++c)
-                        if (lane + 64 * c < A.K) acc[c] += d * fm_field_value(V + (j0 + l) * A.v_stride + lane + 64 * c);
+    // sum over the parts of the candidates, then the teacher's share: thread = (slice of the terms, k)
+    const int width = KP < BS ? KP : BS, slices = BS / width;
+    for (int k0 = 0; k0 < KP; k0 += width) {
+        const int k = k0 + tid % width, slice = tid / width;
+        float s = 0.f;
+        if (counts) {
+            for (int i = slice; i < A.splits; i += slices) {
+                const int64_t at = (int64_t)i * A.n + row;
+                const float4 q = A.part[at];
+                if (q.y != 0.f) s = fmaf(__builtin_amdgcn_exp2f(q.x - p.m), A.opart[at * KP + k], s);
             }
-            __syncthreads();
-        }
-    for (int c = 0; c < 4; ++c)
-        if (lane + 64 * c < A.K) A.grad_G[row * A.K + lane + 64 * c] = acc[c];
-}
-
-// Candidate j: its gradient.  One wavefront to a candidate.
-template <typename TV>
-__global__ __launch_bounds__(64) void k_field_distill_cols(const FieldArgs A)
-{
-    const int lane = threadIdx.x;
-    const int64_t j = blockIdx.x;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, gw = 0.f;
-    for (int64_t i0 = 0; i0 < A.n; i0 += 64) {
-        const int64_t row = i0 + lane;
-        float d = 0.f;
-        if (row < A.n) {
-            const float4 info = A.rows[row];
-            if (info.y != 0.f) {
-                const float z = fm_field_logit<TV>(A, row, A.G + row * A.g_stride, j);
-                if (z != -INFINITY) {
-                    d = __builtin_amdgcn_exp2f(fmaf(z, A.sl, -info.x)) * info.y;
-                    for (int t = 0; t < A.T; ++t)
-                        if (A.ids[row * A.T + t] == j)
-                            d -= __builtin_amdgcn_exp2f(A.teacher[row * A.T + t] * A.sl - info.z) * info.w;
+            s *= rs;
+            for (int t = slice; t < A.T; t += slices)
+                if (entry(t, z) && k < A.K) {
+                    const float q = __builtin_amdgcn_exp2f(teacher[t] * A.sl - mt) * (r / Q);
+                    s = fmaf(-q, fm_field_value(V + (int64_t)ids[t] * A.v_stride + k), s);
                 }
-            }
         }
-        gw += d;
-        for (int l = 0; l < 64; ++l) {
-            const float dl = __shfl(d, l);
-            if (dl != 0.f)
-                for (int c = 0; c < 4; ++c)
-                    if (lane + 64 * c < A.K) acc[c] += dl * A.G[(i0 + l) * A.g_stride + lane + 64 * c];
+        __syncthreads();
+        wide[tid] = s;
+        __syncthreads();
+        if (slice == 0 && k < A.K) {
+            for (int i = 1; i < slices; ++i) s += wide[tid + i * width];
+            A.grad_G[row * A.K + k] = nan && counts ? NAN : s;
         }
     }
-    for (int x = 32; x > 0; x >>= 1) gw += __shfl_xor(gw, x);
-    if (A.grad_w != nullptr && lane == 0) A.grad_w[j] = gw;
-    if (A.grad_V != nullptr)
-        for (int c = 0; c < 4; ++c)
-            if (lane + 64 * c < A.K) A.grad_V[j * A.K + lane + 64 * c] = acc[c];
 }
 
-constexpr int FIELD_SLOTS = 4096;                     // wavefronts that the rows of a small call are split into
+constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most and if there is as much to do
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
+constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
+constexpr int FIELD_HIT_WORDS = 512;                     // words of bits to a tile of rows, at most
 
 }  // namespace
 
@@ -322,9 +287,10 @@ struct fm_field {
     int64_t C, max_rows;
     int32_t K, max_top;
     int device;
-    char* block;      // the workspace
-    int64_t slots;    // FieldParts in it
-    int64_t top_rows; // rows whose group maxima fit
+    char* block;       // the workspace
+    int64_t slots;     // parts of rows (FieldPart and sum of candidates) in it
+    int64_t col_parts; // parts of candidates
+    int64_t top_rows;  // rows whose group maxima fit
     char err[256];
 };
 
@@ -344,10 +310,45 @@ int fail(fm_field* f, int code, const char* fmt, ...)
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t room(int64_t bytes) { return (size_t)up(bytes, 256) * 256; }
 
-int32_t splits_of(const fm_field* f, int64_t n)
+int64_t whole16(int64_t n) { return up(n, 16) * 16; }
+int32_t padded(int32_t K) { return 16 * fm_field_chunks(K); }
+
+// Blocks of 64 candidates or more, so many that their bits fit FIELD_HIT_WORDS.
+int32_t hit_shift(int64_t C)
 {
-    return (int32_t)std::max<int64_t>(1, std::min(up(FIELD_SLOTS, n), up(f->C, FM_GROUP)));
+    int32_t s = 6;
+    while (up(C, int64_t(1) << s) > 32 * FIELD_HIT_WORDS) ++s;
+    return s;
 }
+int32_t hit_words(int64_t C) { return (int32_t)up(up(C, int64_t(1) << hit_shift(C)), 32); }
+
+// Where the pieces of the workspace begin.  The maxima of groups (logprobs) and what distillation needs share their place.
+struct Layout {
+    size_t part, gmax, opart, rm, rs, rq, g0, gs, hits, wpart, vpart, bytes;
+    explicit Layout(const fm_field* f)
+    {
+        size_t at = 0;
+        const auto take = [&](int64_t bytes) {
+            const size_t here = at;
+            at += room(bytes);
+            return here;
+        };
+        const int64_t KP = padded(f->K), rows = whole16(f->max_rows);
+        part = take(f->slots * 16);
+        gmax = opart = at;
+        const size_t top = at + room(f->top_rows * up(f->C, FM_GROUP) * 4);
+        take(f->slots * KP * 4);
+        rm = take(rows * 4);
+        rs = take(rows * 4);
+        rq = take(rows * 8);
+        g0 = take(rows * KP * 4);
+        gs = take(rows * KP * 4);
+        hits = take(rows / 16 * hit_words(f->C) * 4);
+        wpart = take(f->col_parts * 4);
+        vpart = take(f->col_parts * KP * 4);
+        bytes = std::max(at, top);
+    }
+};
 
 int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
 {
@@ -370,7 +371,7 @@ int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_
     return FM_OK;
 }
 
-FieldArgs arguments(const fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
+FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
 {
     FieldArgs A = {};
     A.V = c->V;
@@ -385,12 +386,32 @@ FieldArgs arguments(const fm_field* f, const fm_candidates* c, int64_t n, const 
     A.n = (int32_t)n;
     A.scale = c->scale;
     A.sl = c->scale * FM_LOG2E;
-    A.splits = splits_of(f, n);
-    A.chunk = up(up(f->C, A.splits), FM_GROUP) * FM_GROUP;
+    const int64_t per = fm_field_rows_per_wave(distill, f->K, n);
+    A.row_tiles = (int32_t)up(n, per);
+    const int64_t splits = std::max<int64_t>(1, std::min(FIELD_ITEMS / std::max(A.row_tiles, 1), (int32_t)std::min<int64_t>(up(f->C, FM_GROUP), INT32_MAX)));
+    A.chunk = up(up(f->C, splits), FM_GROUP) * FM_GROUP;
     A.splits = (int32_t)up(f->C, A.chunk);
-    A.part = reinterpret_cast<float4*>(f->block);
-    A.rows = reinterpret_cast<float4*>(f->block + room(f->slots * 16));
     A.ngroups = up(f->C, FM_GROUP);
+    const Layout at(f);
+    const auto floats = [&](size_t where) { return reinterpret_cast<float*>(f->block + where); };
+    A.part = reinterpret_cast<float4*>(f->block + at.part);
+    A.gmax = floats(at.gmax);
+    A.opart = floats(at.opart);
+    A.rm = floats(at.rm);
+    A.rs = floats(at.rs);
+    A.rq = reinterpret_cast<float2*>(f->block + at.rq);
+    A.g0 = floats(at.g0);
+    A.gs = floats(at.gs);
+    A.hits = reinterpret_cast<uint32_t*>(f->block + at.hits);
+    A.wpart = floats(at.wpart);
+    A.vpart = floats(at.vpart);
+    A.npad = (int32_t)whole16(n);
+    A.hit_shift = hit_shift(f->C);
+    A.hit_words = hit_words(f->C);
+    A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 16));
+    A.row_chunk = (int32_t)std::max<int64_t>(16, up(up(A.npad, parts), 16) * 16);
+    A.row_splits = (int32_t)std::max<int64_t>(1, up(A.npad, A.row_chunk));
     return A;
 }
 
@@ -429,9 +450,13 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     f->K = K;
     f->max_rows = max_rows;
     f->max_top = max_top;
-    f->slots = max_rows + FIELD_SLOTS;
+    // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
+    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, INT32_MAX)), max_rows * up(C, FM_GROUP));
+    const int64_t tiles = up(C, fm_field_cols_per_wave(K));
+    const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole16(max_rows) / 16);
+    f->col_parts = col_parts > 1 ? C * col_parts : 0;  // a single part is written to where it belongs
     f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / up(C, FM_GROUP)));
-    const size_t bytes = room(f->slots * 16) + room(max_rows * 16) + room(f->top_rows * up(C, FM_GROUP) * 4);
+    const size_t bytes = Layout(f).bytes;
     hipError_t e = hipGetDevice(&f->device);
     if (e == hipSuccess) e = hipMalloc((void**)&f->block, bytes);
     if (e != hipSuccess) {  // what closed handles left may be what is missing
@@ -467,9 +492,9 @@ extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n,
     if (n == 0) return FM_OK;
     hipStream_t st = (hipStream_t)hip_stream;
     if (top_ids == nullptr && top_logprob == nullptr) top = 0;
-    const int64_t step = top > 0 ? f->top_rows : n;
+    const int64_t step = std::min(top > 0 ? f->top_rows : n, FIELD_MOST_ROWS);
     for (int64_t at = 0; at < n; at += step) {
-        FieldArgs A = arguments(f, c, std::min(step, n - at), G + at * g_stride, g_stride);
+        FieldArgs A = arguments(f, false, c, std::min(step, n - at), G + at * g_stride, g_stride);
         if (A.mask != nullptr) A.mask += at * A.mask_stride;
         A.T = T;
         A.top = top;
@@ -479,10 +504,10 @@ extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n,
         A.entropy = entropy != nullptr ? entropy + at : nullptr;
         A.top_ids = top_ids != nullptr ? top_ids + at * top : nullptr;
         A.top_logprob = top_logprob != nullptr ? top_logprob + at * top : nullptr;
-        A.gmax = top > 0 ? reinterpret_cast<float*>(f->block + room(f->slots * 16) + room(f->max_rows * 16)) : nullptr;
+        if (top == 0) A.gmax = nullptr;
+        fm_field_rows(false, c->v_type, A, st);
         FM_TRY(by_type(c->v_type, [&](auto* t) {
             using TV = std::remove_pointer_t<decltype(t)>;
-            k_field_stats<TV><<<dim3((uint32_t)A.n, (uint32_t)A.splits), 64, 0, st>>>(A);
             k_field_finish<TV, FM_BLOCK><<<(uint32_t)A.n, FM_BLOCK, 0, st>>>(A);
             return launched(f);
         }));
@@ -498,8 +523,8 @@ extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, 
     FM_TRY(check(f, c, n, G, g_stride));
     if (T < 1 || (n > 0 && (ids == nullptr || teacher == nullptr))) return fail(f, FM_EINVAL, "ids and teacher of T=%d >= 1 entries to a row are needed", T);
     hipStream_t st = (hipStream_t)hip_stream;
-    FieldArgs A = arguments(f, c, std::max<int64_t>(n, 1), G, g_stride);
-    A.n = (int32_t)n;
+    if (n > FIELD_MOST_ROWS) return fail(f, FM_ERANGE, "n=%lld: at most %lld rows to a call", (long long)n, (long long)FIELD_MOST_ROWS);
+    FieldArgs A = arguments(f, true, c, n, G, g_stride);
     A.T = T;
     A.ids = ids;
     A.teacher = teacher;
@@ -508,13 +533,14 @@ extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, 
     A.grad_G = grad_G;
     A.grad_V = grad_V;
     A.grad_w = grad_w;
-    return by_type(c->v_type, [&](auto* t) {
-        using TV = std::remove_pointer_t<decltype(t)>;
-        if (n > 0) {
-            k_field_stats<TV><<<dim3((uint32_t)n, (uint32_t)A.splits), 64, 0, st>>>(A);
-            k_field_distill_rows<TV><<<(uint32_t)n, 64, 0, st>>>(A);
-        }
-        if (grad_V != nullptr || grad_w != nullptr) k_field_distill_cols<TV><<<(uint32_t)A.C, 64, 0, st>>>(A);
-        return launched(f);
-    });
+    if (n > 0) {
+        fm_field_rows(true, c->v_type, A, st);
+        FM_TRY(by_type(c->v_type, [&](auto* t) {
+            using TV = std::remove_pointer_t<decltype(t)>;
+            k_field_distill_rows<TV, FM_BLOCK><<<(uint32_t)A.npad, FM_BLOCK, 0, st>>>(A, padded(f->K));
+            return launched(f);
+        }));
+    }
+    if (grad_V != nullptr || grad_w != nullptr) fm_field_cols(c->v_type, A, st);
+    return launched(f);
 }
