@@ -3,11 +3,9 @@
 
 #include "fm_device.h"
 
-// Best candidates are found by way of the largest logit of every FM_GROUP candidates: of the `top` groups with the largest
-// ones (lower groups first among equal ones) every other candidate is behind `top` better ones.  FM_GROUPS such groups
-// make one of a second level.
-constexpr int FM_GROUP = 64;
-constexpr int FM_GROUPS = 64;
+// The sweep over the candidates leaves the largest logit of every group of 16: of block b of FM_BLOCK_CANDS = 64 candidates,
+// group g = 0..3 holds 64 b + 16 i + 4 g + r, i and r = 0..3, which is what one lane has of a row.
+constexpr int FM_BLOCK_CANDS = 64;
 constexpr int FM_FIELD_TOP = 64;
 
 constexpr float FM_LOG2E = 1.44269504088896340736f, FM_LN2 = 0.69314718055994530942f;
@@ -44,11 +42,16 @@ struct FieldArgs {
     float scale, sl;  // sl = scale log2(e)
     // rows against parts of the candidates
     int32_t row_tiles, splits;
-    int64_t chunk;    // candidates to a split, a multiple of FM_GROUP
+    int64_t chunk;    // candidates to a split, a multiple of FM_BLOCK_CANDS
     float4* part;     // [splits][n] FieldPart
     float* opart;     // [splits][n][KP] sum 2^(x - m) v_j (distillation)
-    float* gmax;      // [n][ngroups] largest logit of every group, or nullptr
-    int64_t ngroups;
+    float* gmax;      // [n][blocks][4] largest logit of every group, or nullptr
+    int64_t blocks;
+    // V and w laid out for the matrix cores, if there are rows enough to pay for it
+    bool packed;
+    uint4* pv;        // [candidates / 16][NV][64 lanes] operands of the logits
+    uint4* pt;        // [candidates / 32][KC][NP][64 lanes] operands of the sum of candidates, finite
+    float* pw;        // [candidates] w; -infinity for those that no row allows and beyond C
     // logprobs
     const int32_t* ids;
     float *logprob, *lse, *entropy, *top_logprob;
@@ -57,15 +60,15 @@ struct FieldArgs {
     // distillation
     const float *teacher, *weight;
     float *loss, *grad_G, *grad_V, *grad_w;
-    int32_t npad;     // n in whole tiles of 16 rows
+    int32_t npad;     // n in whole tiles of 32 rows
     float* rm;        // [npad] reference m of the row's exponentials
     float* rs;        // [npad] weight scale / S; 0: no part in the gradient
     float2* rq;       // [npad] largest scaled teacher logit; S / Q, the share of the teacher in units of the exponentials
-    float* g0;        // [npad][KP] G, 0 for rows without a part in the gradient, NaN for rows that are NaN
-    float* gs;        // [npad][KP] rs G, finite
-    uint32_t* hits;   // [npad / 16][hit_words] blocks of 2^hit_shift candidates that some row of the tile names
+    uint4* g0;        // [npad / 16][NG][64 lanes] operands of G: 0 for rows without a part in the gradient, NaN for rows that are NaN
+    uint4* gs;        // [npad / 32][KC][3][64 lanes] operands of rs G, finite
+    uint32_t* hits;   // [npad / 32][hit_words] blocks of 2^hit_shift candidates that some row of the tile names
     int32_t hit_words, hit_shift;
-    int32_t col_tiles, row_splits, row_chunk;  // candidates against parts of the rows, multiples of 16 rows
+    int32_t col_tiles, row_splits, row_chunk;  // candidates against parts of the rows, multiples of 32 rows
     float* vpart;     // [row_splits][C][KP] parts of grad_V, and [row_splits][C] of grad_w
     float* wpart;
 };
@@ -79,13 +82,27 @@ __device__ __forceinline__ bool fm_field_allowed(const FieldArgs& A, int64_t row
     return A.mask == nullptr || (A.mask[row * A.mask_stride + (j >> 5)] >> (j & 31) & 1u) != 0;
 }
 
-// Logit of candidate j in a row: -infinity where it is not allowed.
+template <typename T> struct FmUnaligned4;
+template <> struct FmUnaligned4<float> { typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
+template <> struct FmUnaligned4<_Float16> { typedef _Float16 type __attribute__((ext_vector_type(4), aligned(2))); };
+template <> struct FmUnaligned4<__bf16> { typedef __bf16 type __attribute__((ext_vector_type(4), aligned(2))); };
+
+// Logit of candidate j in a row with aggregates g (in LDS, 16-byte aligned): -infinity where it is not allowed.
 template <typename TV>
 __device__ __forceinline__ float fm_field_logit(const FieldArgs& A, int64_t row, const float* g, int64_t j)
 {
     if (!fm_field_allowed(A, row, j)) return -INFINITY;
     const TV* v = static_cast<const TV*>(A.V) + j * A.v_stride;
-    float z = A.w != nullptr ? A.w[j] : 0.f;
-    for (int k = 0; k < A.K; ++k) z = fmaf(g[k], fm_field_value(v + k), z);
-    return z;
+    float z = 0.f;
+    int k = 0;
+    for (; k + 4 <= A.K; k += 4) {
+        const auto x = *reinterpret_cast<const typename FmUnaligned4<TV>::type*>(v + k);
+        const float4 y = *reinterpret_cast<const float4*>(g + k);
+        z = fmaf(y.x, (float)x[0], z);
+        z = fmaf(y.y, (float)x[1], z);
+        z = fmaf(y.z, (float)x[2], z);
+        z = fmaf(y.w, (float)x[3], z);
+    }
+    for (; k < A.K; ++k) z = fmaf(g[k], fm_field_value(v + k), z);
+    return fmaf(z, 0.f, z) + (A.w != nullptr ? A.w[j] : 0.f);  // infinite values of G and V count as NaN
 }

@@ -20,19 +20,6 @@ __device__ __forceinline__ uint32_t logit_key(float z)
 
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k & 0x7FFFFFFFu : ~k); }
 
-template <int X>
-__device__ __forceinline__ uint64_t max_xor(uint64_t v)
-{
-    const uint32_t lo = (uint32_t)fm_xor_lane<X>((int)(uint32_t)v), hi = (uint32_t)fm_xor_lane<X>((int)(uint32_t)(v >> 32));
-    const uint64_t o = (uint64_t)hi << 32 | lo;
-    return o > v ? o : v;
-}
-
-__device__ __forceinline__ uint64_t wave_max(uint64_t v)
-{
-    return max_xor<1>(max_xor<2>(max_xor<4>(max_xor<8>(max_xor<16>(max_xor<32>(v))))));
-}
-
 // Statistics of a row over all splits, the same in all threads of the workgroup.
 template <int BS>
 __device__ __forceinline__ FieldPart row_stats(const FieldArgs& A, int64_t row, FieldPart* lds)
@@ -53,133 +40,226 @@ __device__ __forceinline__ FieldPart row_stats(const FieldArgs& A, int64_t row, 
     return p;
 }
 
-// Largest key below `below` that `key_at` gives for the items 0..count-1, keys being (order of the value, item counted from
-// the end), so that lower items come first among equal values.  0: none.  The same in all threads.
-template <int BS, typename F>
-__device__ __forceinline__ uint64_t next_best(int64_t count, uint64_t& mine, uint64_t below, uint64_t* lds, F key_at)
-{
-    if (mine >= below) {  // the thread's best was taken, or it has not looked yet
-        mine = 0;
-        for (int64_t i = threadIdx.x; i < count; i += BS) {
-            const uint64_t k = key_at(i);
-            if (k < below && k > mine) mine = k;
-        }
-    }
-    uint64_t best = wave_max(mine);
-    if constexpr (BS > 64) {
-        __syncthreads();
-        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = best;
-        __syncthreads();
-        best = lds[0];
-        for (int i = 1; i < BS / 64; ++i) best = lds[i] > best ? lds[i] : best;
-    }
-    return best;
-}
-
-__device__ __forceinline__ uint64_t item_key(float z, int64_t i)
+// Order of an item of value z and number id: by value, lower numbers first among equal ones.  0: never among the best.
+__device__ __forceinline__ uint64_t item_key(float z, int64_t id)
 {
     const uint32_t k = logit_key(z);
-    return k == 0 ? 0 : (uint64_t)k << 32 | (uint32_t)~(uint32_t)i;
+    return k == 0 ? 0 : (uint64_t)k << 32 | (uint32_t)~(uint32_t)id;
+}
+__device__ __forceinline__ int64_t key_id(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
+
+// The `top` largest keys of 4 * quads items into best[0..top), in order, 0 from where there are no more.  values(q) are the
+// values of items 4 q..4 q + 3, number(q) is the number of the first of them.  Items go to 64 buckets; what is below the
+// top-th largest of the buckets' maxima is not among the best, and of what is not (a few more than `top` if the order of the items has
+// nothing to do with the buckets), everyone counts who is before it.  Where that is more than the list holds, the best are
+// taken one by one.  Ends with a barrier.
+constexpr int SELECT_LIST = 512;
+template <int BS>
+struct SelectLds {
+    uint64_t max[BS], list[SELECT_LIST], from;
+    int count;
+};
+
+template <int BS, typename F, typename N>
+__device__ __forceinline__ void select_best(int64_t quads, int top, uint64_t* best, SelectLds<BS>& lds, F values, N number)
+{
+    const int tid = threadIdx.x;
+    const auto each = [&](auto take) {
+        for (int64_t q = tid; q < quads; q += BS) {
+            const float4 v = values(q);
+            const int64_t id = number(q);
+            take(v.x, id);
+            take(v.y, id + 1);
+            take(v.z, id + 2);
+            take(v.w, id + 3);
+        }
+    };
+    uint64_t mine = 0;
+    each([&](float z, int64_t id) {
+        const uint64_t k = item_key(z, id);
+        mine = k > mine ? k : mine;
+    });
+    lds.max[tid] = mine;
+    if (tid == 0) lds.count = 0, lds.from = 1;
+    for (int a = tid; a < top; a += BS) best[a] = 0;
+    __syncthreads();
+    if (tid < 64) {
+        for (int i = tid + 64; i < BS; i += 64) mine = lds.max[i] > mine ? lds.max[i] : mine;
+        lds.list[tid] = mine;
+    }
+    __syncthreads();
+    if (tid < 64) {
+        int before = 0;
+#pragma unroll 8
+        for (int i = 0; i < 64; ++i) before += lds.list[i] > mine;
+        if (mine != 0 && before == top - 1) lds.from = mine;
+    }
+    __syncthreads();
+    const uint64_t from = lds.from;
+    each([&](float z, int64_t id) {
+        const uint64_t k = item_key(z, id);
+        if (k >= from) {
+            const int at = atomicAdd(&lds.count, 1);
+            if (at < SELECT_LIST) lds.list[at] = k;
+        }
+    });
+    __syncthreads();
+    const int count = lds.count;
+    if (count <= SELECT_LIST) {
+        for (int i = tid; i < count; i += BS) {
+            const uint64_t k = lds.list[i];
+            int before = 0;
+            for (int o = 0; o < count; ++o) before += lds.list[o] > k;
+            if (before < top) best[before] = k;
+        }
+    } else {
+        uint64_t below = ~0ull;
+        for (int a = 0; a < top && below != 0; ++a) {
+            mine = 0;
+            each([&](float z, int64_t id) {
+                const uint64_t k = item_key(z, id);
+                mine = k < below && k > mine ? k : mine;
+            });
+            lds.max[tid] = mine;
+            __syncthreads();
+            for (int i = 0; i < BS; ++i) mine = lds.max[i] > mine ? lds.max[i] : mine;
+            __syncthreads();
+            below = mine;
+            if (tid == 0) best[a] = mine;
+        }
+    }
+    __syncthreads();
 }
 
 // What is left of a row: its sums joined, given candidates, best candidates.
 template <typename TV, int BS>
 __global__ __launch_bounds__(BS) void k_field_finish(const FieldArgs A)
 {
-    __shared__ float g[256];
+    __shared__ __align__(16) float g[256];
     __shared__ FieldPart parts[BS / 64];
-    __shared__ uint64_t best[BS / 64];
-    __shared__ int32_t groups[FM_FIELD_TOP];
-    __shared__ float zs[FM_FIELD_TOP * FM_GROUP];
+    const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
-    for (int k = threadIdx.x; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
+    for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
     const FieldPart p = row_stats<BS>(A, row, parts);
     __syncthreads();
-    const bool empty = p.S == 0.f;
+    const bool empty = p.S == 0.f, nan = p.S != p.S;
     const float log2S = __builtin_amdgcn_logf(p.S);
-    if (threadIdx.x == 0) {
+    if (tid == 0) {
         if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
         if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
     }
     const auto logprob = [&](float z) {
-        return p.S != p.S ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
+        return nan ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
     };
     if (A.logprob != nullptr)
-        for (int t = threadIdx.x; t < A.T; t += BS) {
+        for (int t = tid; t < A.T; t += BS) {
             const int64_t j = A.ids[row * A.T + t];
             A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
         }
-    if (A.gmax == nullptr) return;
-    // candidates: groups of groups, of these the groups, of these the candidates
-    const float* gm = A.gmax + row * A.ngroups;
-    const bool nan = p.S != p.S;
-    uint64_t mine = ~0ull, below = ~0ull;
-    int nsel = 0;
-    const int64_t nsuper = (A.ngroups + FM_GROUPS - 1) / FM_GROUPS;
-    for (; !nan && nsel < A.top; ++nsel) {
-        below = next_best<BS>(nsuper, mine, below, best, [&](int64_t i) {
-            float z = -INFINITY;
-            for (int64_t q = i * FM_GROUPS; q < min(A.ngroups, (i + 1) * FM_GROUPS); ++q) z = fmaxf(z, gm[q]);
-            return item_key(z, i);
-        });
-        if (below == 0) break;
-        if (threadIdx.x == 0) groups[nsel] = (int32_t)~(uint32_t)below;
+}
+
+// The same with the best candidates: the groups with the `top` largest maxima hold them (lower blocks first among equal
+// ones, all groups of a block that are equal to the last), and the logits of these groups are computed once more.
+template <typename TV, int BS>
+__global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
+{
+    extern __shared__ __align__(16) float zs[];  // [4 top][16]
+    __shared__ __align__(16) float g[256];
+    __shared__ FieldPart parts[BS / 64];
+    __shared__ SelectLds<BS> lds;
+    __shared__ uint64_t best[FM_FIELD_TOP];
+    __shared__ int32_t groups[4 * FM_FIELD_TOP], ngroups;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
+    const FieldPart p = row_stats<BS>(A, row, parts);
+    __syncthreads();
+    const bool empty = p.S == 0.f, nan = p.S != p.S;
+    const float log2S = __builtin_amdgcn_logf(p.S);
+    if (tid == 0) {
+        if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
+        if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
+        ngroups = 0;
+    }
+    const auto logprob = [&](float z) {
+        return nan ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
+    };
+    if (A.logprob != nullptr)
+        for (int t = tid; t < A.T; t += BS) {
+            const int64_t j = A.ids[row * A.T + t];
+            A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
+        }
+    const float4* gm = reinterpret_cast<const float4*>(A.gmax) + row * A.blocks;
+    select_best<BS>(nan ? 0 : A.blocks, A.top, best, lds, [&](int64_t q) { return gm[q]; }, [](int64_t q) { return 4 * q; });
+    for (int i = tid; i < 4 * A.top; i += BS) {
+        const uint64_t k = best[i / 4];
+        if (k == 0) continue;
+        const int64_t id = key_id(k), other = id / 4 * 4 + i % 4;
+        bool take = other == id;
+        if (!take) {  // equal to the last one that was taken, and not taken itself
+            const float4 v = gm[id / 4];
+            const uint64_t last = best[A.top - 1], mine = item_key(i % 4 == 0 ? v.x : i % 4 == 1 ? v.y : i % 4 == 2 ? v.z : v.w, other);
+            take = last != 0 && mine < last && mine >> 32 == last >> 32;
+            for (int o = 0; take && o < i / 4; ++o) take = best[o] == 0 || key_id(best[o]) / 4 != id / 4;  // once for the block
+        }
+        if (take) groups[atomicAdd(&ngroups, 1)] = (int32_t)other;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < nsel * FM_GROUPS; i += BS) {
-        const int64_t q = (int64_t)groups[i / FM_GROUPS] * FM_GROUPS + i % FM_GROUPS;
-        zs[i] = q < A.ngroups ? gm[q] : -INFINITY;
-    }
-    __syncthreads();
-    const int nq = nsel * FM_GROUPS;
-    // the groups taken are in the order of their maxima, not of their numbers: keys are made of the numbers
-    mine = below = ~0ull;
-    nsel = 0;
-    int32_t taken = 0;  // of thread a: the a-th group taken
-    for (; !nan && nsel < A.top; ++nsel) {
-        below = next_best<BS>(nq, mine, below, best, [&](int64_t i) {
-            return item_key(zs[i], (int64_t)groups[i / FM_GROUPS] * FM_GROUPS + i % FM_GROUPS);
-        });
-        if (below == 0) break;
-        if (threadIdx.x == nsel) taken = (int32_t)~(uint32_t)below;
-    }
-    __syncthreads();
-    if ((int)threadIdx.x < nsel) groups[threadIdx.x] = taken;
-    __syncthreads();
-    for (int i = threadIdx.x; i < nsel * FM_GROUP; i += BS) {
-        const int64_t j = (int64_t)groups[i / FM_GROUP] * FM_GROUP + i % FM_GROUP;
+    const int ng = ngroups;
+    const auto first = [&](int64_t q) {  // of four consecutive candidates: 16 i of group q / 4
+        const int64_t id = groups[q / 4];
+        return id / 4 * FM_BLOCK_CANDS + 16 * (q % 4) + 4 * (id % 4);
+    };
+    for (int i = tid; i < 16 * ng; i += BS) {
+        const int64_t j = first(i / 4) + i % 4;
         zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
     }
     __syncthreads();
-    const int nj = nsel * FM_GROUP;
-    mine = below = ~0ull;
-    for (int a = 0; a < A.top; ++a) {
-        if (below != 0 && nj > 0)
-            below = next_best<BS>(nj, mine, below, best, [&](int64_t i) {
-                return item_key(zs[i], (int64_t)groups[i / FM_GROUP] * FM_GROUP + i % FM_GROUP);
-            });
-        else
-            below = 0;
-        if (threadIdx.x == 0) {
-            const bool none = below == 0;
-            if (A.top_ids != nullptr) A.top_ids[row * A.top + a] = none ? -1 : (int32_t)~(uint32_t)below;
-            if (A.top_logprob != nullptr)
-                A.top_logprob[row * A.top + a] = nan ? NAN : none ? -INFINITY : logprob(key_logit((uint32_t)(below >> 32)));
-        }
+    select_best<BS>(4 * ng, A.top, best, lds, [&](int64_t q) { return reinterpret_cast<const float4*>(zs)[q]; }, first);
+    for (int a = tid; a < A.top; a += BS) {
+        const uint64_t k = best[a];
+        if (A.top_ids != nullptr) A.top_ids[row * A.top + a] = k == 0 ? -1 : (int32_t)key_id(k);
+        if (A.top_logprob != nullptr)
+            A.top_logprob[row * A.top + a] = nan ? NAN : k == 0 ? -INFINITY : logprob(key_logit((uint32_t)(k >> 32)));
     }
 }
 
 // Row i: loss, its gradient by G, and what the candidates need of it.  Rows beyond n, up to a whole tile, are empty ones.
-template <typename TV, int BS>
-__global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A, int32_t KP)
+template <typename TV, int KC, int BS>
+__global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
 {
-    __shared__ float g[256];
+    constexpr int KP = 16 * KC;
+    extern __shared__ float2 entries[];  // [T] logit and scaled teacher logit, then the share of the entry
+    __shared__ __align__(16) float g[256];
     __shared__ FieldPart parts[BS / 64];
     __shared__ float sums[BS / 64], wide[BS];
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
+    // the row's part of the operands: k0..k0 + 3 of G as the logits take it, and of rs G
+    const auto lay_out = [&](int k0, f32x4 x, f32x4 y) {
+        using Ops = FieldOps<FmParts<TV>::value, KC>;
+        const int64_t lane = (k0 % 16 / 4) * 16 + row % 16;
+        bf16x4 p[3];
+        split<3>(x, p);
+        bf16x4* g0 = reinterpret_cast<bf16x4*>(A.g0 + row / 16 * Ops::NG * 64);
+#pragma unroll
+        for (int o = 0; o < Ops::NG; ++o)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (Ops::chunk_of(o, h) == k0 / 16) {
+                    const int q = Ops::part_of(o, h);
+                    g0[(o * 64 + lane) * 2 + h] = q == 0 ? p[0] : q == 1 ? p[1] : q == 2 ? p[2] : bf16x4{};
+                }
+        split<3>(y, p);
+        __bf16* gs = reinterpret_cast<__bf16*>(A.gs + (row / 32 * KC + k0 / 16) * 3 * 64);
+        const int64_t r = row % 32;
+#pragma unroll
+        for (int q = 0; q < 3; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) gs[(q * 64 + r % 16 / 4 * 16 + k0 % 16 + e) * 8 + r / 16 * 4 + r % 4] = p[q][e];
+    };
     if (row >= A.n) {
-        for (int k = tid; k < KP; k += BS) A.g0[row * KP + k] = A.gs[row * KP + k] = 0.f;
+        for (int k = 4 * tid; k < KP; k += 4 * BS) lay_out(k, f32x4{}, f32x4{});
         if (tid == 0) A.rm[row] = 3e38f, A.rs[row] = 0.f, A.rq[row] = make_float2(0.f, 0.f);
         return;
     }
@@ -205,35 +285,39 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A, in
     const TV* V = static_cast<const TV*>(A.V);
     const int32_t* ids = A.ids + row * A.T;
     const float* teacher = A.teacher + row * A.T;
-    const auto entry = [&](int t, float& z) {
+    float x = -INFINITY;
+    for (int t = tid; t < A.T; t += BS) {
         const int64_t j = ids[t];
-        if (j < 0 || j >= A.C) return false;
-        z = fm_field_logit<TV>(A, row, g, j);
-        return z != -INFINITY && teacher[t] != -INFINITY;
-    };
-    float x = -INFINITY, z;
-    for (int t = tid; t < A.T; t += BS)
-        if (entry(t, z)) x = fmaxf(x, teacher[t] * A.sl);
+        float2 e = make_float2(-INFINITY, -INFINITY);
+        if (j >= 0 && j < A.C) e = make_float2(fm_field_logit<TV>(A, row, g, j), teacher[t] * A.sl);
+        if (e.x == -INFINITY) e.y = -INFINITY;
+        entries[t] = e;
+        x = fmaxf(x, e.y);
+    }
     const float mt = block(x, true);
     x = 0.f;
     for (int t = tid; t < A.T; t += BS)
-        if (entry(t, z)) x += __builtin_amdgcn_exp2f(teacher[t] * A.sl - mt);
+        if (entries[t].y != -INFINITY) x += __builtin_amdgcn_exp2f(entries[t].y - mt);
     const float Q = block(x, false);
     const bool takes = Q != 0.f, nan = p.S != p.S;
     const float log2Q = __builtin_amdgcn_logf(Q), r = takes ? (A.weight != nullptr ? A.weight[row] : 1.f) * A.scale : 0.f;
     const bool counts = r != 0.f;
     x = 0.f;
-    if (takes)
-        for (int t = tid; t < A.T; t += BS)
-            if (entry(t, z)) {
-                const float y = teacher[t] * A.sl - mt, q = __builtin_amdgcn_exp2f(y) / Q;
-                const float d = (y - log2Q) - (fmaf(z, A.sl, -p.m) - log2S);
-                if (q != 0.f) x += q * d * FM_LN2;
-                if (counts) {
-                    const int64_t block = ids[t] >> A.hit_shift;
-                    atomicOr(A.hits + row / 16 * A.hit_words + (block >> 5), 1u << (block & 31));
-                }
+    for (int t = tid; t < A.T; t += BS) {
+        const float2 e = entries[t];
+        float q = 0.f;
+        if (e.y != -INFINITY) {
+            const float y = e.y - mt;
+            q = __builtin_amdgcn_exp2f(y) / Q;
+            const float d = (y - log2Q) - (fmaf(e.x, A.sl, -p.m) - log2S);
+            if (q != 0.f) x += q * d * FM_LN2;
+            if (counts) {
+                const int64_t at = ids[t] >> A.hit_shift;
+                atomicOr(A.hits + row / 32 * A.hit_words + (at >> 5), 1u << (at & 31));
             }
+        }
+        entries[t] = make_float2(q * r, 0.f);
+    }
     x = block(x, false);
     const float rs = counts ? r / p.S : 0.f;
     if (tid == 0) {
@@ -242,12 +326,18 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A, in
         A.rs[row] = nan ? 0.f : rs;
         A.rq[row] = make_float2(mt, counts && !nan ? p.S / Q : 0.f);
     }
-    for (int k = tid; k < KP; k += BS) {
-        const float v = k < A.K ? g[k] : 0.f;
-        A.g0[row * KP + k] = !counts ? 0.f : nan ? NAN : v;
-        A.gs[row * KP + k] = !counts || nan ? 0.f : rs * v;
+    for (int k = 4 * tid; k < KP; k += 4 * BS) {
+        f32x4 v, y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float x = k + e < A.K ? g[k + e] : 0.f;
+            v[e] = !counts ? 0.f : nan ? NAN : x;
+            y[e] = !counts || nan ? 0.f : rs * x;
+        }
+        lay_out(k, v, y);
     }
     if (A.grad_G == nullptr) return;
+    __syncthreads();
     // sum over the parts of the candidates, then the teacher's share: thread = (slice of the terms, k)
     const int width = KP < BS ? KP : BS, slices = BS / width;
     for (int k0 = 0; k0 < KP; k0 += width) {
@@ -260,11 +350,10 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A, in
                 if (q.y != 0.f) s = fmaf(__builtin_amdgcn_exp2f(q.x - p.m), A.opart[at * KP + k], s);
             }
             s *= rs;
-            for (int t = slice; t < A.T; t += slices)
-                if (entry(t, z) && k < A.K) {
-                    const float q = __builtin_amdgcn_exp2f(teacher[t] * A.sl - mt) * (r / Q);
-                    s = fmaf(-q, fm_field_value(V + (int64_t)ids[t] * A.v_stride + k), s);
-                }
+            for (int t = slice; t < A.T; t += slices) {
+                const float q = entries[t].x;
+                if (q != 0.f && k < A.K) s = fmaf(-q, fm_field_value(V + (int64_t)ids[t] * A.v_stride + k), s);
+            }
         }
         __syncthreads();
         wide[tid] = s;
@@ -279,6 +368,8 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A, in
 constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most and if there is as much to do
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
+constexpr int64_t FIELD_FEW_ROWS = 256;                  // up to so many rows get a workgroup of 1024 threads, others a wavefront
+constexpr int FIELD_MOST_ENTRIES = 4096;                 // of a teacher, to a row
 constexpr int FIELD_HIT_WORDS = 512;                     // words of bits to a tile of rows, at most
 
 }  // namespace
@@ -287,6 +378,7 @@ struct fm_field {
     int64_t C, max_rows;
     int32_t K, max_top;
     int device;
+    bool packs;        // whether there is room for the packed table
     char* block;       // the workspace
     int64_t slots;     // parts of rows (FieldPart and sum of candidates) in it
     int64_t col_parts; // parts of candidates
@@ -310,8 +402,7 @@ int fail(fm_field* f, int code, const char* fmt, ...)
 int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 size_t room(int64_t bytes) { return (size_t)up(bytes, 256) * 256; }
 
-int64_t whole16(int64_t n) { return up(n, 16) * 16; }
-int32_t padded(int32_t K) { return 16 * fm_field_chunks(K); }
+int64_t whole32(int64_t n) { return up(n, 32) * 32; }
 
 // Blocks of 64 candidates or more, so many that their bits fit FIELD_HIT_WORDS.
 int32_t hit_shift(int64_t C)
@@ -324,7 +415,7 @@ int32_t hit_words(int64_t C) { return (int32_t)up(up(C, int64_t(1) << hit_shift(
 
 // Where the pieces of the workspace begin.  The maxima of groups (logprobs) and what distillation needs share their place.
 struct Layout {
-    size_t part, gmax, opart, rm, rs, rq, g0, gs, hits, wpart, vpart, bytes;
+    size_t part, gmax, opart, rm, rs, rq, g0, gs, hits, wpart, vpart, pv, pt, pw, bytes;
     explicit Layout(const fm_field* f)
     {
         size_t at = 0;
@@ -333,22 +424,30 @@ struct Layout {
             at += room(bytes);
             return here;
         };
-        const int64_t KP = padded(f->K), rows = whole16(f->max_rows);
+        const int64_t KC = fm_field_chunks(f->K), KP = 16 * KC, rows = whole32(f->max_rows), cands = up(f->C, FM_BLOCK_CANDS) * FM_BLOCK_CANDS;
         part = take(f->slots * 16);
+        const bool packed = f->packs;
+        pv = take(packed ? cands / 16 * 1024 * (KC == 1 ? 2 : 3 * KC / 2) : 0);
+        pw = take(packed ? cands * 4 : 0);
         gmax = opart = at;
-        const size_t top = at + room(f->top_rows * up(f->C, FM_GROUP) * 4);
+        const size_t top = at + room(f->top_rows * up(f->C, FM_BLOCK_CANDS) * 16);
         take(f->slots * KP * 4);
         rm = take(rows * 4);
         rs = take(rows * 4);
         rq = take(rows * 8);
-        g0 = take(rows * KP * 4);
-        gs = take(rows * KP * 4);
-        hits = take(rows / 16 * hit_words(f->C) * 4);
+        g0 = take(rows / 16 * 1024 * (KC == 1 ? 3 : 3 * KC / 2));
+        gs = take(rows / 32 * 1024 * 3 * KC);
+        hits = take(rows / 32 * hit_words(f->C) * 4);
         wpart = take(f->col_parts * 4);
         vpart = take(f->col_parts * KP * 4);
+        pt = take(packed ? cands / 32 * 1024 * 3 * KC : 0);
         bytes = std::max(at, top);
     }
 };
+
+// Calls with more rows lay the table out first, unless that takes too much room.
+constexpr int64_t FIELD_DIRECT_ROWS = 64;
+constexpr int64_t FIELD_PACK_BYTES = int64_t(1) << 30;
 
 int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
 {
@@ -386,12 +485,13 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.n = (int32_t)n;
     A.scale = c->scale;
     A.sl = c->scale * FM_LOG2E;
-    const int64_t per = fm_field_rows_per_wave(distill, f->K, n);
+    A.packed = f->packs && n > FIELD_DIRECT_ROWS;
+    const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed);
     A.row_tiles = (int32_t)up(n, per);
-    const int64_t splits = std::max<int64_t>(1, std::min(FIELD_ITEMS / std::max(A.row_tiles, 1), (int32_t)std::min<int64_t>(up(f->C, FM_GROUP), INT32_MAX)));
-    A.chunk = up(up(f->C, splits), FM_GROUP) * FM_GROUP;
+    const int64_t splits = std::max<int64_t>(1, std::min(FIELD_ITEMS / std::max(A.row_tiles, 1), (int32_t)std::min<int64_t>(up(f->C, FM_BLOCK_CANDS), INT32_MAX)));
+    A.chunk = up(up(f->C, splits), FM_BLOCK_CANDS) * FM_BLOCK_CANDS;
     A.splits = (int32_t)up(f->C, A.chunk);
-    A.ngroups = up(f->C, FM_GROUP);
+    A.blocks = up(f->C, FM_BLOCK_CANDS);
     const Layout at(f);
     const auto floats = [&](size_t where) { return reinterpret_cast<float*>(f->block + where); };
     A.part = reinterpret_cast<float4*>(f->block + at.part);
@@ -400,17 +500,20 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.rm = floats(at.rm);
     A.rs = floats(at.rs);
     A.rq = reinterpret_cast<float2*>(f->block + at.rq);
-    A.g0 = floats(at.g0);
-    A.gs = floats(at.gs);
+    A.g0 = reinterpret_cast<uint4*>(f->block + at.g0);
+    A.gs = reinterpret_cast<uint4*>(f->block + at.gs);
+    A.pv = reinterpret_cast<uint4*>(f->block + at.pv);
+    A.pt = reinterpret_cast<uint4*>(f->block + at.pt);
+    A.pw = floats(at.pw);
     A.hits = reinterpret_cast<uint32_t*>(f->block + at.hits);
     A.wpart = floats(at.wpart);
     A.vpart = floats(at.vpart);
-    A.npad = (int32_t)whole16(n);
+    A.npad = (int32_t)whole32(n);
     A.hit_shift = hit_shift(f->C);
     A.hit_words = hit_words(f->C);
     A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 16));
-    A.row_chunk = (int32_t)std::max<int64_t>(16, up(up(A.npad, parts), 16) * 16);
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 32));
+    A.row_chunk = (int32_t)std::max<int64_t>(32, up(up(A.npad, parts), 32) * 32);
     A.row_splits = (int32_t)std::max<int64_t>(1, up(A.npad, A.row_chunk));
     return A;
 }
@@ -422,7 +525,7 @@ int launched(fm_field* f)
 }
 
 template <typename F>
-int by_type(int32_t type, F run)
+void by_type(int32_t type, F run)
 {
     switch (type) {
         case FM_TYPE_F16: return run((_Float16*)nullptr);
@@ -450,12 +553,13 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     f->K = K;
     f->max_rows = max_rows;
     f->max_top = max_top;
+    f->packs = max_rows > FIELD_DIRECT_ROWS && fm_field_pack_bytes(true, K, C) <= FIELD_PACK_BYTES;
     // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
-    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, INT32_MAX)), max_rows * up(C, FM_GROUP));
+    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
     const int64_t tiles = up(C, fm_field_cols_per_wave(K));
-    const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole16(max_rows) / 16);
+    const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole32(max_rows) / 32);
     f->col_parts = col_parts > 1 ? C * col_parts : 0;  // a single part is written to where it belongs
-    f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / up(C, FM_GROUP)));
+    f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / (4 * up(C, FM_BLOCK_CANDS))));
     const size_t bytes = Layout(f).bytes;
     hipError_t e = hipGetDevice(&f->device);
     if (e == hipSuccess) e = hipMalloc((void**)&f->block, bytes);
@@ -506,11 +610,15 @@ extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n,
         A.top_logprob = top_logprob != nullptr ? top_logprob + at * top : nullptr;
         if (top == 0) A.gmax = nullptr;
         fm_field_rows(false, c->v_type, A, st);
-        FM_TRY(by_type(c->v_type, [&](auto* t) {
+        by_type(c->v_type, [&](auto* t) {
             using TV = std::remove_pointer_t<decltype(t)>;
-            k_field_finish<TV, FM_BLOCK><<<(uint32_t)A.n, FM_BLOCK, 0, st>>>(A);
-            return launched(f);
-        }));
+            const uint32_t rows = (uint32_t)A.n, lds = (uint32_t)top * 4 * 16 * sizeof(float);
+            if (top == 0)
+                n <= FIELD_FEW_ROWS ? k_field_finish<TV, 1024><<<rows, 1024, 0, st>>>(A) : k_field_finish<TV, 64><<<rows, 64, 0, st>>>(A);
+            else
+                n <= FIELD_FEW_ROWS ? k_field_finish_top<TV, 1024><<<rows, 1024, lds, st>>>(A) : k_field_finish_top<TV, 64><<<rows, 64, lds, st>>>(A);
+        });
+        FM_TRY(launched(f));
     }
     return FM_OK;
 }
@@ -521,6 +629,7 @@ extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, 
 {
     if (f == nullptr) return FM_EINVAL;
     FM_TRY(check(f, c, n, G, g_stride));
+    if (T > FIELD_MOST_ENTRIES) return fail(f, FM_ERANGE, "T=%d: at most %d entries to a row", T, FIELD_MOST_ENTRIES);
     if (T < 1 || (n > 0 && (ids == nullptr || teacher == nullptr))) return fail(f, FM_EINVAL, "ids and teacher of T=%d >= 1 entries to a row are needed", T);
     hipStream_t st = (hipStream_t)hip_stream;
     if (n > FIELD_MOST_ROWS) return fail(f, FM_ERANGE, "n=%lld: at most %lld rows to a call", (long long)n, (long long)FIELD_MOST_ROWS);
@@ -535,11 +644,13 @@ extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, 
     A.grad_w = grad_w;
     if (n > 0) {
         fm_field_rows(true, c->v_type, A, st);
-        FM_TRY(by_type(c->v_type, [&](auto* t) {
-            using TV = std::remove_pointer_t<decltype(t)>;
-            k_field_distill_rows<TV, FM_BLOCK><<<(uint32_t)A.npad, FM_BLOCK, 0, st>>>(A, padded(f->K));
-            return launched(f);
-        }));
+        fm_field_shape(c->v_type, f->K, [&](auto type, auto kc, auto) {
+            using TV = decltype(type);
+            constexpr int KC = decltype(kc)::value;
+            const uint32_t rows = (uint32_t)A.npad, lds = (uint32_t)T * sizeof(float2);
+            n <= FIELD_FEW_ROWS ? k_field_distill_rows<TV, KC, 1024><<<rows, 1024, lds, st>>>(A)
+                                : k_field_distill_rows<TV, KC, 64><<<rows, 64, lds, st>>>(A);
+        });
     }
     if (grad_V != nullptr || grad_w != nullptr) fm_field_cols(c->v_type, A, st);
     return launched(f);

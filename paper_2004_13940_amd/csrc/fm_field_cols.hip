@@ -11,77 +11,80 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// A wavefront takes 16 NT candidates and a part of the rows, 16 of them at a time.  The tile of logits has rows down and
-// candidates across, so that it is the B operand of the second product (rows are what it sums over) as it stands:
+// A wavefront takes 16 NT candidates and a part of the rows, 32 of them at a time.  The tiles of logits have rows down and
+// candidates across, so that they are the B operand of the second product (rows are what it sums over) as they stand:
 //   grad_V^T[k][j] += gs[i][k] P[i][j],   P_ij = 2^(x_ij - m_i) - (share of the teacher),   gs = weight scale / S G.
 // The teacher's few entries come into the tile by way of LDS, in tiles that have a bit set for their block of candidates.
-template <typename TV, int KC, bool FULL, int NT>
+template <typename TV, int KC, int FILL, int NT>
 __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
 {
-    constexpr int KP = 16 * KC, QS = 20;  // QS: floats to a candidate of the tile in LDS, 16 rows
+    constexpr int NP = FmParts<TV>::value, KP = 16 * KC, QS = 36;  // QS: floats to a candidate of the tile in LDS, 32 rows
+    using Ops = FieldOps<NP, KC>;
     __shared__ __align__(16) float teacher[FM_WAVES][16 * NT * QS];
     const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
     const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     if (item >= (int64_t)A.col_tiles * A.row_splits) return;
     const int64_t c0 = item % A.col_tiles * (16 * NT);
-    const int split = (int)(item / A.col_tiles);
-    const int beg = split * A.row_chunk, end = min(A.npad, beg + A.row_chunk);
+    const int split_no = (int)(item / A.col_tiles);
+    const int beg = split_no * A.row_chunk, end = min(A.npad, beg + A.row_chunk);
     const TV* V = static_cast<const TV*>(A.V);
     float* Q = teacher[threadIdx.x / 64];
     for (int i = lane; i < 16 * NT * QS; i += 64) Q[i] = 0.f;
     wave_sync();
 
-    float b[NT][KC][4], w[NT], gw[NT];
-    f32x4 acc[KC][NT];
+    bf16x8 b[NT][Ops::NV];
+    f32x4 w[NT], acc[KC][NT];
+    float gw[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int64_t j = min(c0 + 16 * t + lo, A.C - 1);
-#pragma unroll
-        for (int c = 0; c < KC; ++c) load4<TV, FULL>(V + j * A.v_stride, 16 * c + 4 * g, A.K, b[t][c]);
-        w[t] = A.w != nullptr ? A.w[j] : 0.f;
+        const bool out = A.mask != nullptr && A.mask_stride == 0 && (A.mask[j >> 5] >> (j & 31) & 1u) == 0;  // of all rows
+        const float wj = out ? -INFINITY : A.w != nullptr ? A.w[j] : 0.f;
+        w[t] = f32x4{wj, wj, wj, wj};
         gw[t] = 0.f;
-        if (A.mask != nullptr && A.mask_stride == 0 && (A.mask[j >> 5] >> (j & 31) & 1u) == 0) {  // left out of all rows
-            w[t] = -INFINITY;
+        bf16x4 p[KC][NP];
 #pragma unroll
-            for (int c = 0; c < KC; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) b[t][c][e] = 0.f;
+        for (int c = 0; c < KC; ++c) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (!out) load4<TV, FILL>(V + j * A.v_stride, 16 * c + 4 * g, A.K, v);
+            finite_or_nan(v);
+            split<NP>(f32x4{v[0], v[1], v[2], v[3]}, p[c]);
+            acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-#pragma unroll
-        for (int c = 0; c < KC; ++c) acc[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        Ops::of_v(p, b[t]);
     }
     const bool row_masks = A.mask != nullptr && A.mask_stride != 0;
     const uint32_t* hits = A.hits + (c0 >> A.hit_shift >> 5);
     const uint32_t hit = 1u << (c0 >> A.hit_shift & 31);
 
-    for (int i0 = beg; i0 < end; i0 += 16) {
-        f32x4 z[NT];
+    for (int i0 = beg; i0 < end; i0 += 32) {
+        f32x4 z[2][NT], m[2], rs[2];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) z[t] = f32x4{w[t], w[t], w[t], w[t]};
+        for (int h = 0; h < 2; ++h) {
+            bf16x8 a[Ops::NG];
 #pragma unroll
-        for (int c = 0; c < KC; ++c) {
-            const f32x4 a = *reinterpret_cast<const f32x4*>(A.g0 + (int64_t)(i0 + lo) * KP + 16 * c + 4 * g);
+            for (int o = 0; o < Ops::NG; ++o) a[o] = __builtin_bit_cast(bf16x8, A.g0[((int64_t)(i0 / 16 + h) * Ops::NG + o) * 64 + lane]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) z[t] = mfma4(a[e], b[t][c][e], z[t]);
+            for (int t = 0; t < NT; ++t) z[h][t] = Ops::template product<false>(b[t], a, w[t]);
+            m[h] = *reinterpret_cast<const f32x4*>(A.rm + i0 + 16 * h + 4 * g);
+            rs[h] = *reinterpret_cast<const f32x4*>(A.rs + i0 + 16 * h + 4 * g);
         }
         if (row_masks) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const uint32_t* words = A.mask + min(i0 + 4 * g + r, A.n - 1) * A.mask_stride;
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int64_t j = min(c0 + 16 * t + lo, A.C - 1);
-                    z[t][r] = words[j >> 5] >> (j & 31) & 1u ? z[t][r] : -INFINITY;
+                for (int r = 0; r < 4; ++r) {
+                    const uint32_t* words = A.mask + min(i0 + 16 * h + 4 * g + r, A.n - 1) * A.mask_stride;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        const int64_t j = min(c0 + 16 * t + lo, A.C - 1);
+                        z[h][t][r] = words[j >> 5] >> (j & 31) & 1u ? z[h][t][r] : -INFINITY;
+                    }
                 }
-            }
         }
-        const f32x4 m = *reinterpret_cast<const f32x4*>(A.rm + i0 + 4 * g);
-        const f32x4 rs = *reinterpret_cast<const f32x4*>(A.rs + i0 + 4 * g);
-        const bool named = (hits[(int64_t)(i0 / 16) * A.hit_words] & hit) != 0;  // the same in all lanes
-        if (named) {
-            for (int i = lane; i < 16 * A.T; i += 64) {
+        const auto exponential = [&](int h, int t, int r) { return __builtin_amdgcn_exp2f(fmaf(z[h][t][r], A.sl, -m[h][r])); };
+        if (hits[(int64_t)(i0 / 32) * A.hit_words] & hit) {  // the same in all lanes
+            for (int i = lane; i < 32 * A.T; i += 64) {
                 const int row = i0 + i / A.T;
                 if (row >= A.n) break;
                 const int64_t j = A.ids[(int64_t)row * A.T + i % A.T] - c0;
@@ -91,31 +94,47 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
                 atomicAdd(&Q[j * QS + i / A.T], share);  // into zero but for ids that come twice
             }
             wave_sync();
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    f32x4* at = reinterpret_cast<f32x4*>(Q + (16 * t + lo) * QS + 16 * h + 4 * g);
+                    const f32x4 q = *at;
+                    *at = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[h][t][r] = exponential(h, t, r) - (z[h][t][r] == -INFINITY ? 0.f : q[r]);
+                }
+            wave_sync();
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) z[h][t][r] = exponential(h, t, r);
         }
+        bf16x8 e[NT][3];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            f32x4 q = {0.f, 0.f, 0.f, 0.f};
-            if (named) {
-                f32x4* at = reinterpret_cast<f32x4*>(Q + (16 * t + lo) * QS + 4 * g);
-                q = *at;
-                *at = f32x4{0.f, 0.f, 0.f, 0.f};
+            bf16x4 x[2][3];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) gw[t] = fmaf(rs[h][r], z[h][t][r], gw[t]);
+                split<3>(z[h][t], x[h]);
             }
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                float e = __builtin_amdgcn_exp2f(fmaf(z[t][r], A.sl, -m[r]));
-                if (named) e -= z[t][r] == -INFINITY ? 0.f : q[r];
-                gw[t] = fmaf(rs[r], e, gw[t]);
-                z[t][r] = e;
-            }
+            for (int q = 0; q < 3; ++q) e[t][q] = join(x[0][q], x[1][q]);
         }
-        if (named) wave_sync();
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int c = 0; c < KC; ++c)
 #pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                const float a = A.gs[(int64_t)(i0 + 4 * g + r) * KP + 16 * c + lo];
+            for (int p = 2; p >= 0; --p) {
+                const bf16x8 a = __builtin_bit_cast(bf16x8, A.gs[((int64_t)(i0 / 32 * KC + c) * 3 + p) * 64 + lane]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[c][t] = mfma4(a, z[t][r], acc[c][t]);
+                for (int q = 2 - p; q >= 0; --q)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) acc[c][t] = mfma32(a, e[t][q], acc[c][t]);
             }
     }
 
@@ -134,13 +153,13 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
                         const int k = 16 * c + 4 * g + r;
-                        if (FULL || k < A.K) A.grad_V[j * A.K + k] = acc[c][t][r];
+                        if (FILL == FILL_WHOLE || k < A.K) A.grad_V[j * A.K + k] = acc[c][t][r];
                     }
         } else {
-            if (g == 0) A.wpart[(int64_t)split * A.C + j] = s;
+            if (g == 0) A.wpart[(int64_t)split_no * A.C + j] = s;
 #pragma unroll
             for (int c = 0; c < KC; ++c)
-                *reinterpret_cast<f32x4*>(A.vpart + ((int64_t)split * A.C + j) * KP + 16 * c + 4 * g) = acc[c][t];
+                *reinterpret_cast<f32x4*>(A.vpart + ((int64_t)split_no * A.C + j) * KP + 16 * c + 4 * g) = acc[c][t];
         }
     }
 }
@@ -171,9 +190,9 @@ int fm_field_cols_per_wave(int32_t K) { return 16 * fm_field_col_tiles(fm_field_
 void fm_field_cols(int32_t v_type, const FieldArgs& A, hipStream_t st)
 {
     const int64_t items = (int64_t)A.col_tiles * A.row_splits;
-    fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto full) {
+    fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto fill) {
         constexpr int KC = decltype(kc)::value;
-        k_field_cols<decltype(type), KC, decltype(full)::value, fm_field_col_tiles(KC)>
+        k_field_cols<decltype(type), KC, decltype(fill)::value, fm_field_col_tiles(KC)>
             <<<(uint32_t)((items + FM_WAVES - 1) / FM_WAVES), FM_BLOCK, 0, st>>>(A);
     });
     if (A.row_splits == 1) return;

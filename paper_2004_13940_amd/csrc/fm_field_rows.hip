@@ -4,20 +4,131 @@
 
 namespace {
 
+// Running statistics of 16 NT rows, of each row a quarter of the candidates to a lane: reference m of the exponentials, which
+// follows the maximum only when that has risen by more than 2^8 over it, S and U as in FieldPart, and for distillation the
+// sums o of the candidates, of which the four lanes of a row hold the latent values 16 c + 4 g + r.
+template <int KC, int NT, bool DISTILL>
+struct RowStats {
+    float m[NT], S[NT], U[NT];
+    f32x4 o[DISTILL ? KC : 1][NT];
+
+    __device__ __forceinline__ RowStats()
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            m[t] = -3e38f;
+            S[t] = U[t] = 0.f;
+#pragma unroll
+            for (int c = 0; c < (DISTILL ? KC : 1); ++c) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // New logits of a block of 64 candidates: maxima out, reference raised if need be.
+    __device__ __forceinline__ void meet(const f32x4 (&z)[4][NT], float sl, float (&top)[NT])
+    {
+        bool rise = false;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float x = fmaxf(fmaxf(z[0][t][0], z[0][t][1]), z[0][t][2]);
+            x = fmaxf(fmaxf(x, z[0][t][3]), z[1][t][0]);
+            x = fmaxf(fmaxf(x, z[1][t][1]), z[1][t][2]);
+            x = fmaxf(fmaxf(x, z[1][t][3]), z[2][t][0]);
+            x = fmaxf(fmaxf(x, z[2][t][1]), z[2][t][2]);
+            x = fmaxf(fmaxf(x, z[2][t][3]), z[3][t][0]);
+            x = fmaxf(fmaxf(x, z[3][t][1]), z[3][t][2]);
+            top[t] = fmaxf(x, z[3][t][3]);
+            rise |= top[t] * sl > m[t] + 8.f;
+        }
+        if (!__any(rise)) return;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            float to = fmaxf(m[t], top[t] * sl);
+            if constexpr (DISTILL) {
+                to = fmaxf(to, fm_xor_lane<16>(to));
+                to = fmaxf(to, fm_xor_lane<32>(to));
+            }
+            const float d = m[t] - to, f = __builtin_amdgcn_exp2f(d);
+            if constexpr (!DISTILL) U[t] = f > 0.f ? f * (U[t] + d * S[t]) : 0.f;
+            S[t] *= f;
+            m[t] = to;
+            if constexpr (DISTILL)
+#pragma unroll
+                for (int c = 0; c < KC; ++c) o[c][t] *= f;
+        }
+    }
+
+    // Exponentials of a tile, summed; for distillation they take the place of the logits.
+    __device__ __forceinline__ void take(f32x4& z, int t, float sl)
+    {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const float x = fmaf(z[r], sl, -m[t]), e = __builtin_amdgcn_exp2f(x);
+            S[t] += e;
+            if constexpr (DISTILL)
+                z[r] = e;
+            else
+                U[t] = fmaf(e, fmaxf(x, -200.f), U[t]);  // e is 0 where x is -infinity
+        }
+    }
+
+    __device__ __forceinline__ void leave(const FieldArgs& A, int split, int row0, int lo, int g)
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int row = row0 + 16 * t + lo;
+            FieldPart p = {m[t], S[t], U[t]};
+            p = fm_field_merge(p, {fm_xor_lane<16>(p.m), fm_xor_lane<16>(p.S), fm_xor_lane<16>(p.U)});
+            p = fm_field_merge(p, {fm_xor_lane<32>(p.m), fm_xor_lane<32>(p.S), fm_xor_lane<32>(p.U)});
+            if (row >= A.n) continue;
+            const int64_t at = (int64_t)split * A.n + row;
+            if (g == 0) A.part[at] = make_float4(p.m, p.S, p.U, 0.f);
+            if constexpr (DISTILL)
+#pragma unroll
+                for (int c = 0; c < KC; ++c) *reinterpret_cast<f32x4*>(A.opart + at * 16 * KC + 16 * c + 4 * g) = o[c][t];
+        }
+    }
+};
+
+// -infinity for what the mask words of a row leave out of a block: bits[h] are candidates 32 h..32 h + 31 of it.
+template <int NT>
+__device__ __forceinline__ void leave_out(f32x4 (&z)[4][NT], int t, const uint32_t (&bits)[2], int g)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t four = bits[i / 2] >> (16 * (i % 2) + 4 * g);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) z[i][t][r] = four >> r & 1u ? z[i][t][r] : -INFINITY;
+    }
+}
+
+template <int NT>
+__device__ __forceinline__ void store_maxima(const FieldArgs& A, const float (&top)[NT], int row0, int64_t block, int lo, int g)
+{
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row0 + 16 * t + lo;
+        if (row < A.n) A.gmax[(row * A.blocks + block) * 4 + g] = top[t];
+    }
+}
+
+// Bits that k_field_distill_rows sets.
+__device__ __forceinline__ void clear_hits(const FieldArgs& A)
+{
+    const int64_t words = (int64_t)(A.npad / 32) * A.hit_words;
+    for (int64_t i = (int64_t)blockIdx.x * FM_BLOCK + threadIdx.x; i < words; i += (int64_t)gridDim.x * FM_BLOCK) A.hits[i] = 0;
+}
+
 // A wavefront takes 16 NT rows and a part of the candidates, 16 of them at a time.  The tile of logits has candidates down
 // and rows across, so that a lane has four candidates of one row of every 16: maxima and sums stay in the lane, and the tile
-// is the B operand of the second product (candidates are what it sums over) as it stands.
-// The reference m of the exponentials follows the maximum only when that has risen by more than 2^8 over it.
-template <typename TV, int KC, bool FULL, int NT, bool DISTILL>
-__global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows(const FieldArgs A)
+// is the B operand of the second product (candidates are what it sums over) as it stands.  fp32 products straight from V:
+// for calls with so few rows that laying V out would cost more than it saves.
+template <typename TV, int KC, int FILL, int NT, bool DISTILL>
+__global__ __launch_bounds__(FM_BLOCK, KC == 16 ? 1 : 2) void k_field_rows(const FieldArgs A)
 {
     constexpr int KP = 16 * KC;
     const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
     const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if constexpr (DISTILL) {  // the bits that the next kernel sets
-        const int64_t words = (int64_t)(A.npad / 16) * A.hit_words;
-        for (int64_t i = (int64_t)blockIdx.x * FM_BLOCK + threadIdx.x; i < words; i += (int64_t)gridDim.x * FM_BLOCK) A.hits[i] = 0;
-    }
+    if constexpr (DISTILL) clear_hits(A);
     if (item >= (int64_t)A.row_tiles * A.splits) return;
     const int split = (int)(item / A.row_tiles), row0 = (int)(item % A.row_tiles) * 16 * NT;
     const int64_t beg = split * A.chunk, end = min(A.C, beg + A.chunk);
@@ -30,26 +141,23 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows(const FieldArgs A)
         const int64_t row = min(row0 + 16 * t + lo, A.n - 1);
         mask_row[t] = row * A.mask_stride;
 #pragma unroll
-        for (int c = 0; c < KC; ++c) load4<float, FULL>(A.G + row * A.g_stride, 16 * c + 4 * g, A.K, b[t][c]);
+        for (int c = 0; c < KC; ++c) {
+            load4<float, FILL>(A.G + row * A.g_stride, 16 * c + 4 * g, A.K, b[t][c]);
+            finite_or_nan(b[t][c]);
+        }
     }
-    float m[NT], S[NT], U[NT];
-    f32x4 o[DISTILL ? KC : 1][NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        m[t] = -3e38f;
-        S[t] = U[t] = 0.f;
-#pragma unroll
-        for (int c = 0; c < (DISTILL ? KC : 1); ++c) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    for (int64_t j0 = beg; j0 < end; j0 += FM_GROUP) {
+    RowStats<KC, NT, DISTILL> s;
+    for (int64_t j0 = beg; j0 < end; j0 += FM_BLOCK_CANDS) {
         f32x4 z[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float a[KC][4];
             const TV* v = V + min(j0 + 16 * i + lo, A.C - 1) * A.v_stride;
 #pragma unroll
-            for (int c = 0; c < KC; ++c) load4<TV, FULL>(v, 16 * c + 4 * g, A.K, a[c]);
+            for (int c = 0; c < KC; ++c) {
+                load4<TV, FILL>(v, 16 * c + 4 * g, A.K, a[c]);
+                finite_or_nan(a[c]);
+            }
             f32x4 w = {0.f, 0.f, 0.f, 0.f};
             if (A.w != nullptr)
 #pragma unroll
@@ -63,7 +171,7 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows(const FieldArgs A)
 #pragma unroll
                     for (int t = 0; t < NT; ++t) z[i][t] = mfma4(a[c][e], b[t][c][e], z[i][t]);
         }
-        if (A.mask != nullptr || j0 + FM_GROUP > end) {
+        if (A.mask != nullptr || j0 + FM_BLOCK_CANDS > end) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 uint32_t bits[2];
@@ -73,69 +181,16 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows(const FieldArgs A)
                     bits[h] = left <= 0 ? 0u : left < 32 ? (1u << left) - 1u : ~0u;
                     if (A.mask != nullptr && left > 0) bits[h] &= A.mask[mask_row[t] + (j0 >> 5) + h];
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t four = bits[i / 2] >> (16 * (i % 2) + 4 * g);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[i][t][r] = four >> r & 1u ? z[i][t][r] : -INFINITY;
-                }
+                leave_out(z, t, bits, g);
             }
         }
         float top[NT];
-        bool rise = false;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            float x = fmaxf(fmaxf(z[0][t][0], z[0][t][1]), z[0][t][2]);
-            x = fmaxf(fmaxf(x, z[0][t][3]), z[1][t][0]);
-            x = fmaxf(fmaxf(x, z[1][t][1]), z[1][t][2]);
-            x = fmaxf(fmaxf(x, z[1][t][3]), z[2][t][0]);
-            x = fmaxf(fmaxf(x, z[2][t][1]), z[2][t][2]);
-            x = fmaxf(fmaxf(x, z[2][t][3]), z[3][t][0]);
-            x = fmaxf(fmaxf(x, z[3][t][1]), z[3][t][2]);
-            top[t] = fmaxf(x, z[3][t][3]);
-            rise |= top[t] * A.sl > m[t] + 8.f;
-        }
-        if (!DISTILL && A.gmax != nullptr) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                float x = fmaxf(top[t], fm_xor_lane<16>(top[t]));
-                x = fmaxf(x, fm_xor_lane<32>(x));
-                const int row = row0 + 16 * t + lo;
-                if (g == 0 && row < A.n) A.gmax[row * A.ngroups + j0 / FM_GROUP] = x;
-            }
-        }
-        if (__any(rise)) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                float to = fmaxf(m[t], top[t] * A.sl);
-                if constexpr (DISTILL) {  // the four lanes of a row share its sums of candidates
-                    to = fmaxf(to, fm_xor_lane<16>(to));
-                    to = fmaxf(to, fm_xor_lane<32>(to));
-                }
-                const float d = m[t] - to, f = __builtin_amdgcn_exp2f(d);
-                if constexpr (!DISTILL) U[t] = f > 0.f ? f * (U[t] + d * S[t]) : 0.f;
-                S[t] *= f;
-                m[t] = to;
-                if constexpr (DISTILL)
-#pragma unroll
-                    for (int c = 0; c < KC; ++c)
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) o[c][t][r] *= f;
-            }
-        }
+        s.meet(z, A.sl, top);
+        if (!DISTILL && A.gmax != nullptr) store_maxima(A, top, row0, j0 / FM_BLOCK_CANDS, lo, g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = fmaf(z[i][t][r], A.sl, -m[t]), e = __builtin_amdgcn_exp2f(x);
-                    S[t] += e;
-                    if constexpr (DISTILL)
-                        z[i][t][r] = e;
-                    else
-                        U[t] = fmaf(e, fmaxf(x, -200.f), U[t]);  // e is 0 where x is -infinity
-                }
+            for (int t = 0; t < NT; ++t) s.take(z[i][t], t, A.sl);
             if constexpr (DISTILL) {
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
@@ -143,54 +198,187 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows(const FieldArgs A)
 #pragma unroll
                     for (int c = 0; c < KC; ++c) {
                         // what is left out has probability 0, which is to stay 0 whatever its values are
-                        const float a = finite(FULL || 16 * c + lo < A.K ? fm_field_value(v + 16 * c + lo) : 0.f);
+                        const float a = finite(FILL == FILL_WHOLE || 16 * c + lo < A.K ? fm_field_value(v + 16 * c + lo) : 0.f);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) o[c][t] = mfma4(a, z[i][t][r], o[c][t]);
+                        for (int t = 0; t < NT; ++t) s.o[c][t] = mfma4(a, z[i][t][r], s.o[c][t]);
                     }
                 }
             }
         }
     }
+    s.leave(A, split, row0, lo, g);
+}
 
+// Lays V and w out: a wavefront to 32 candidates.
+template <typename TV, int KC, int FILL, bool DISTILL>
+__global__ __launch_bounds__(FM_BLOCK) void k_field_pack(const FieldArgs A)
+{
+    constexpr int NP = FmParts<TV>::value;
+    using Ops = FieldOps<NP, KC>;
+    const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
+    const int64_t tile = (int64_t)blockIdx.x * FM_WAVES + threadIdx.x / 64;
+    if (tile >= A.blocks * 2) return;
+    const bool shared = A.mask != nullptr && A.mask_stride == 0;
+    const TV* V = static_cast<const TV*>(A.V);
+    const auto there = [&](int64_t j) { return j < A.C && (!shared || (A.mask[j >> 5] >> (j & 31) & 1u) != 0); };
+    if (lane < 32) {
+        const int64_t j = tile * 32 + lane;
+        A.pw[j] = !there(j) ? -INFINITY : A.w != nullptr ? A.w[j] : 0.f;
+    }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = row0 + 16 * t + lo;
-        FieldPart p = {m[t], S[t], U[t]};
-        p = fm_field_merge(p, {fm_xor_lane<16>(p.m), fm_xor_lane<16>(p.S), fm_xor_lane<16>(p.U)});
-        p = fm_field_merge(p, {fm_xor_lane<32>(p.m), fm_xor_lane<32>(p.S), fm_xor_lane<32>(p.U)});
-        if (row >= A.n) continue;
-        const int64_t at = (int64_t)split * A.n + row;
-        if (g == 0) A.part[at] = make_float4(p.m, p.S, p.U, 0.f);
-        if constexpr (DISTILL)
+    for (int h = 0; h < 2; ++h) {
+        const int64_t j = tile * 32 + 16 * h + lo;
+        bf16x4 p[KC][NP];
+        bf16x8 ops[Ops::NV];
 #pragma unroll
-            for (int c = 0; c < KC; ++c) *reinterpret_cast<f32x4*>(A.opart + at * KP + 16 * c + 4 * g) = o[c][t];
+        for (int c = 0; c < KC; ++c) {
+            float v[4] = {0.f, 0.f, 0.f, 0.f};
+            if (there(j)) load4<TV, FILL>(V + j * A.v_stride, 16 * c + 4 * g, A.K, v);
+            finite_or_nan(v);
+            split<NP>(f32x4{v[0], v[1], v[2], v[3]}, p[c]);
+        }
+        Ops::of_v(p, ops);
+#pragma unroll
+        for (int o = 0; o < Ops::NV; ++o) A.pv[((tile * 2 + h) * Ops::NV + o) * 64 + lane] = __builtin_bit_cast(uint4, ops[o]);
+    }
+    if constexpr (DISTILL) {
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            bf16x4 p[2][NP];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4 v;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int64_t j = tile * 32 + 16 * h + 4 * g + r;
+                    const int k = 16 * c + lo;
+                    // what is left out has probability 0, which is to stay 0 whatever its values are
+                    v[r] = there(j) && k < A.K ? finite(fm_field_value(V + j * A.v_stride + k)) : 0.f;
+                }
+                split<NP>(v, p[h]);
+            }
+#pragma unroll
+            for (int q = 0; q < NP; ++q)
+                A.pt[((tile * KC + c) * NP + q) * 64 + lane] = __builtin_bit_cast(uint4, join(p[0][q], p[1][q]));
+        }
     }
 }
 
-template <typename TV, int KC, bool FULL, int NT, bool DISTILL>
-void launch(const FieldArgs& A, hipStream_t st)
+// The same as k_field_rows from the packed table, products as sums of bfloat16 ones.
+template <int NP, int KC, int NT, bool DISTILL>
+__global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldArgs A)
 {
-    const int64_t items = (int64_t)A.row_tiles * A.splits;
-    k_field_rows<TV, KC, FULL, NT, DISTILL><<<(uint32_t)((items + FM_WAVES - 1) / FM_WAVES), FM_BLOCK, 0, st>>>(A);
+    using Ops = FieldOps<NP, KC>;
+    const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
+    const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if constexpr (DISTILL) clear_hits(A);
+    if (item >= (int64_t)A.row_tiles * A.splits) return;
+    const int split_no = (int)(item / A.row_tiles), row0 = (int)(item % A.row_tiles) * 16 * NT;
+    const int64_t beg = split_no * A.chunk, end = min(A.C, beg + A.chunk);
+    const bool row_masks = A.mask != nullptr && A.mask_stride != 0;
+
+    bf16x8 b[NT][Ops::NG];
+    int64_t mask_row[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t row = min(row0 + 16 * t + lo, A.n - 1);
+        mask_row[t] = row * A.mask_stride;
+        bf16x4 p[KC][3];
+#pragma unroll
+        for (int c = 0; c < KC; ++c) {
+            float x[4];
+            load4<float, FILL_ANY>(A.G + row * A.g_stride, 16 * c + 4 * g, A.K, x);
+            finite_or_nan(x);
+            split<3>(f32x4{x[0], x[1], x[2], x[3]}, p[c]);
+        }
+        Ops::of_g(p, b[t]);
+    }
+    RowStats<KC, NT, DISTILL> s;
+    for (int64_t j0 = beg; j0 < end; j0 += FM_BLOCK_CANDS) {
+        f32x4 z[4][NT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x8 a[Ops::NV];
+#pragma unroll
+            for (int o = 0; o < Ops::NV; ++o) a[o] = __builtin_bit_cast(bf16x8, A.pv[((j0 / 16 + i) * Ops::NV + o) * 64 + lane]);
+            const f32x4 w = *reinterpret_cast<const f32x4*>(A.pw + j0 + 16 * i + 4 * g);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) z[i][t] = Ops::template product<true>(a, b[t], w);
+        }
+        if (row_masks) {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                uint32_t bits[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) bits[h] = j0 + 32 * h < A.C ? A.mask[mask_row[t] + (j0 >> 5) + h] : 0u;
+                leave_out(z, t, bits, g);
+            }
+        }
+        float top[NT];
+        s.meet(z, A.sl, top);
+        if (!DISTILL && A.gmax != nullptr) store_maxima(A, top, row0, j0 / FM_BLOCK_CANDS, lo, g);
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            bf16x8 e[NT][3];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                s.take(z[i][t], t, A.sl);
+                s.take(z[i + 1][t], t, A.sl);
+                if constexpr (DISTILL) {
+                    bf16x4 x[3], y[3];
+                    split<3>(z[i][t], x);
+                    split<3>(z[i + 1][t], y);
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) e[t][q] = join(x[q], y[q]);
+                }
+            }
+            if constexpr (DISTILL) {
+#pragma unroll
+                for (int c = 0; c < KC; ++c)
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) {
+                        const bf16x8 a = __builtin_bit_cast(bf16x8, A.pt[(((j0 + 16 * i) / 32 * KC + c) * NP + p) * 64 + lane]);
+#pragma unroll
+                        for (int q = 2 - p; q >= 0; --q)
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) s.o[c][t] = mfma32(a, e[t][q], s.o[c][t]);
+                    }
+            }
+        }
+    }
+    s.leave(A, split_no, row0, lo, g);
 }
+
+uint32_t blocks_of(int64_t wavefronts) { return (uint32_t)((wavefronts + FM_WAVES - 1) / FM_WAVES); }
 
 template <bool DISTILL>
 void rows(int32_t v_type, const FieldArgs& A, hipStream_t st)
 {
-    fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto full) {
+    fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto fill) {
         using TV = decltype(type);
-        constexpr int KC = decltype(kc)::value;
-        constexpr bool FULL = decltype(full)::value;
-        if (A.n <= 16) return launch<TV, KC, FULL, 1, DISTILL>(A, st);
-        launch<TV, KC, FULL, fm_field_row_tiles(KC, DISTILL), DISTILL>(A, st);
+        constexpr int KC = decltype(kc)::value, FILL = decltype(fill)::value;
+        const uint32_t grid = blocks_of((int64_t)A.row_tiles * A.splits);
+        if (A.packed) {
+            k_field_pack<TV, KC, FILL, DISTILL><<<blocks_of(A.blocks * 2), FM_BLOCK, 0, st>>>(A);
+            k_field_rows_packed<FmParts<TV>::value, KC, fm_field_row_tiles(KC, DISTILL), DISTILL><<<grid, FM_BLOCK, 0, st>>>(A);
+        } else {
+            k_field_rows<TV, KC, FILL, 1, DISTILL><<<grid, FM_BLOCK, 0, st>>>(A);
+        }
     });
 }
 
 }  // namespace
 
-int fm_field_rows_per_wave(bool distill, int32_t K, int64_t n)
+int fm_field_rows_per_wave(bool distill, int32_t K, bool packed)
 {
-    return n <= 16 ? 16 : 16 * fm_field_row_tiles(fm_field_chunks(K), distill);
+    return packed ? 16 * fm_field_row_tiles(fm_field_chunks(K), distill) : 16;
+}
+
+int64_t fm_field_pack_bytes(bool distill, int32_t K, int64_t C)
+{
+    const int KC = fm_field_chunks(K);
+    const int64_t cands = (C + FM_BLOCK_CANDS - 1) / FM_BLOCK_CANDS * FM_BLOCK_CANDS;
+    return cands / 16 * 1024 * (KC == 1 ? 2 : 3 * KC / 2) + (distill ? cands / 32 * 1024 * 3 * KC : 0) + cands * 4;
 }
 
 void fm_field_rows(bool distill, int32_t v_type, const FieldArgs& A, hipStream_t st)

@@ -11,50 +11,142 @@
 #include "fm_field.h"
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4_unaligned __attribute__((ext_vector_type(4), aligned(4)));
-typedef _Float16 f16x4_unaligned __attribute__((ext_vector_type(4), aligned(2)));
-typedef __bf16 bf16x4_unaligned __attribute__((ext_vector_type(4), aligned(2)));
-
 __device__ __forceinline__ f32x4 mfma4(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// fp32 products from bfloat16 ones (v_mfma_f32_16x16x32_bf16, 16 times the rate).  A value is the sum of three bfloat16
+// parts, each the rounded rest of the ones before it: x = x0 + x1 + x2 to 2^-24, |x1| <= 2^-8 |x|, |x2| <= 2^-16 |x|, a half
+// precision value of two, a bfloat16 one of one.  Of the products of parts those with x_p y_q, p + q <= 2, are taken; the
+// others are below 2^-24 of the whole.
+// A lane holds 8 of the 32 values that an instruction sums over, twice 4: the four it has of a chunk of 16 latent values, of
+// two chunks, or, where there is one chunk only, of two parts (KC = 1: the products of all parts fill whole instructions).
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+template <int PARTS>
+__device__ __forceinline__ void split(f32x4 x, bf16x4 (&p)[PARTS])
+{
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        p[i] = __builtin_convertvector(x, bf16x4);
+        if (i + 1 < PARTS) x -= __builtin_convertvector(p[i], f32x4);
+    }
+}
+__device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+
+template <typename TV> struct FmParts { static constexpr int value = std::is_same_v<TV, float> ? 3 : std::is_same_v<TV, _Float16> ? 2 : 1; };
+
+// Operands of <G_i, v_j> over the KC chunks: NV of the parts of V, NG of those of G.
+template <int NP, int KC>
+struct FieldOps {
+    static constexpr int NV = KC == 1 ? (NP == 3 ? 2 : 1) : NP * KC / 2;
+    static constexpr int NG = KC == 1 ? (NP == 1 ? 2 : 3) : 3 * KC / 2;
+
+    static __device__ __forceinline__ void of_v(const bf16x4 (&v)[KC][NP], bf16x8 (&a)[NV])
+    {
+        if constexpr (KC == 1) {
+            a[0] = join(v[0][0], v[0][NP == 1 ? 0 : 1]);
+            if constexpr (NP == 3) a[1] = join(v[0][2], v[0][0]);
+        } else {
+#pragma unroll
+            for (int c = 0; c < KC; c += 2)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) a[c / 2 * NP + p] = join(v[c][p], v[c + 1][p]);
+        }
+    }
+    // Operand o holds in half h (its values 4 h..4 h + 3) part part_of(o, h) of chunk chunk_of(o, h); part 3: zeros.
+    static constexpr __host__ __device__ int part_of(int o, int h)
+    {
+        if (KC > 1) return o % 3;
+        if (NP == 1) return 2 * o + h;  // x0 x1 | x2 0, against v v
+        return NP == 3 && o == 2 ? (h == 0 ? 0 : 2) : o;  // x0 x0 | x1 x1 | x0 x2, against v0 v1 and v2 v0; x2 x2 against v0 v1
+    }
+    static constexpr __host__ __device__ int chunk_of(int o, int h) { return KC > 1 ? o / 3 * 2 + h : 0; }
+
+    static __device__ __forceinline__ void of_g(const bf16x4 (&g)[KC][3], bf16x8 (&b)[NG])
+    {
+#pragma unroll
+        for (int o = 0; o < NG; ++o) {
+            bf16x4 x[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (part_of(o, h) < 3)
+                    x[h] = g[chunk_of(o, h)][part_of(o, h) % 3];
+                else
+                    x[h] = bf16x4{};
+            }
+            b[o] = join(x[0], x[1]);
+        }
+    }
+    // V_DOWN: candidates down, rows across; else the other way round.
+    template <bool V_DOWN>
+    static __device__ __forceinline__ f32x4 product(const bf16x8 (&v)[NV], const bf16x8 (&g)[NG], f32x4 c)
+    {
+        const auto add = [&](bf16x8 x, bf16x8 y) { c = V_DOWN ? mfma32(x, y, c) : mfma32(y, x, c); };
+        if constexpr (KC == 1) {
+            if constexpr (NP == 3) add(v[1], g[2]);
+            if constexpr (NP == 2) add(v[0], g[2]);
+            add(v[0], g[1]);
+            add(v[0], g[0]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < KC / 2; ++k)
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int q = 2 - p; q >= 0; --q) add(v[k * NP + p], g[k * 3 + q]);
+        }
+        return c;
+    }
+};
 
 // The nearest finite value: times a probability of 0 it is 0.
 __device__ __forceinline__ float finite(float v) { return __builtin_amdgcn_fmed3f(v, -FLT_MAX, FLT_MAX); }
 
-template <typename T> struct Unaligned4;
-template <> struct Unaligned4<float> { using type = f32x4_unaligned; };
-template <> struct Unaligned4<_Float16> { using type = f16x4_unaligned; };
-template <> struct Unaligned4<__bf16> { using type = bf16x4_unaligned; };
+// Infinite values count as NaN.
+__device__ __forceinline__ void finite_or_nan(float (&v)[4])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(v[e], 0.f, v[e]);
+}
 
-// Values k..k+3 of a row of K; 0 beyond.  FULL: there is nothing beyond.
-template <typename T, bool FULL>
+// How K fills whole chunks of 16: entirely, in quads, in single values.
+enum { FILL_ANY = 0, FILL_QUADS = 1, FILL_WHOLE = 2 };
+
+// Values k..k+3 of a row of K, k % 4 == 0; 0 beyond.
+template <typename T, int FILL>
 __device__ __forceinline__ void load4(const T* row, int k, int K, float (&v)[4])
 {
-    if constexpr (FULL) {
-        const auto x = *reinterpret_cast<const typename Unaligned4<T>::type*>(row + k);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = (float)x[e];
-    } else {
+    if constexpr (FILL == FILL_ANY) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = k + e < K ? (float)row[k + e] : 0.f;
+    } else {
+        const bool there = FILL == FILL_WHOLE || k < K;
+        const auto x = *reinterpret_cast<const typename FmUnaligned4<T>::type*>(row + (there ? k : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = there ? (float)x[e] : 0.f;
     }
 }
 
 // Chunks of 16 latent values that the kernels for K have: 1, 2, 4, 8 or 16.
 constexpr int fm_field_chunks(int32_t K) { return K <= 16 ? 1 : K <= 32 ? 2 : K <= 64 ? 4 : K <= 128 ? 8 : 16; }
 // Tiles of 16 rows, or of 16 candidates, that stay in a wavefront's registers: 256 of them are to do.
-constexpr int fm_field_row_tiles(int KC, bool distill) { return KC <= (distill ? 2 : 4) ? 4 : KC <= 8 ? 2 : 1; }
-constexpr int fm_field_col_tiles(int KC) { return KC <= 4 ? 4 : KC == 8 ? 2 : 1; }
+constexpr int fm_field_row_tiles(int KC, bool distill) { return KC <= (distill ? 1 : 2) ? 4 : KC <= (distill ? 4 : 8) ? 2 : 1; }
+constexpr int fm_field_col_tiles(int KC) { return KC <= 1 ? 4 : KC <= 4 ? 2 : 1; }
 
 template <int V> using IntC = std::integral_constant<int, V>;
 
-// Calls run(a value of V's type, chunks, whether K fills them).
+// Calls run(a value of V's type, chunks, how K fills them).
 template <typename F>
 void fm_field_shape(int32_t v_type, int32_t K, F run)
 {
     const auto by_k = [&](auto type) {
         const int kc = fm_field_chunks(K);
-        const bool full = K == 16 * kc;
-        const auto of = [&](auto chunks) { full ? run(type, chunks, std::true_type{}) : run(type, chunks, std::false_type{}); };
+        const auto of = [&](auto chunks) {
+            if (K == 16 * kc) return run(type, chunks, IntC<FILL_WHOLE>{});
+            K % 4 == 0 ? run(type, chunks, IntC<FILL_QUADS>{}) : run(type, chunks, IntC<FILL_ANY>{});
+        };
         switch (kc) {
             case 1: return of(IntC<1>{});
             case 2: return of(IntC<2>{});
@@ -70,7 +162,8 @@ void fm_field_shape(int32_t v_type, int32_t K, F run)
     }
 }
 
-int fm_field_rows_per_wave(bool distill, int32_t K, int64_t n);
-void fm_field_rows(bool distill, int32_t v_type, const FieldArgs& A, hipStream_t st);
+int fm_field_rows_per_wave(bool distill, int32_t K, bool packed);
+void fm_field_rows(bool distill, int32_t v_type, const FieldArgs& A, hipStream_t st);  // through the packed table where A.packed
 int fm_field_cols_per_wave(int32_t K);
+int64_t fm_field_pack_bytes(bool distill, int32_t K, int64_t C);  // of the largest type
 void fm_field_cols(int32_t v_type, const FieldArgs& A, hipStream_t st);
