@@ -244,10 +244,11 @@ int fm_get_aux(const fm_matrix* m, float* a /*N*/, float* G /*N*K*/, float* q /*
  * field of a block of columns.  A candidate is allowed in a row if its bit in the row's mask is set (all are without a mask)
  * and its logit is above -infinity; whatever stands in V and w at candidates that no row allows is not part of any result.
  * The logits are never stored: n and C may be such that n C values would not fit.  Sums and probabilities are fp32.
- * A row with an allowed logit that is NaN or +infinity gets NaN for all of its values (top_ids -1).
+ * A row with an allowed logit that is NaN or +infinity gets NaN for all of its values (top_ids -1); infinite values in G and V
+ * count as NaN.
  *
- * The handle holds workspace for calls of up to max_rows rows and max_top best candidates (0..64), on the device that is
- * current when it is made.  Calls allocate nothing, never wait for the stream and may be captured into a graph; two calls
+ * The handle holds workspace for calls of up to max_rows rows, max_top best candidates (0..64) and max_entries entries of a
+ * teacher to a row (0..4096; 0: fm_field_logprobs only), on the device that is current when it is made.  Calls allocate nothing, never wait for the stream and may be captured into a graph; two calls
  * on one handle must not overlap in time.  1 <= C < 2^31, K as in fm_params, 1 <= max_rows < 2^31. */
 typedef struct fm_field fm_field;
 
@@ -264,7 +265,7 @@ typedef struct {
     float scale;          /* 1 / temperature, positive and finite */
 } fm_candidates;
 
-int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t max_top, fm_field** out);
+int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t max_top, int32_t max_entries, fm_field** out);
 int fm_field_destroy(fm_field* f);
 const char* fm_field_last_error(const fm_field* f); /* f may be NULL: last creation error of this thread */
 
@@ -280,7 +281,7 @@ int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n, const floa
                       float* entropy /*DEVICE n*/, int32_t top, int32_t* top_ids /*DEVICE n*top*/,
                       float* top_logprob /*DEVICE n*top*/, void* hip_stream);
 
-/* Distillation from a teacher's T largest logits of every row, 1 <= T <= 4096, n <= 2^22; entries with ids outside [0, C),
+/* Distillation from a teacher's T largest logits of every row, 1 <= T <= max_entries, n <= 2^22; entries with ids outside [0, C),
  * such that the row does not allow and with a logit of -infinity are left out, the ids of a row are distinct (the shares
  * of equal ones add up).
  *   q_it   = softmax over the entries of a row of scale * teacher_it

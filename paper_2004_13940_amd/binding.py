@@ -81,7 +81,7 @@ def load() -> ctypes.CDLL:
                 "fm_minibatch_epoch": [vp] * 8, "fm_stratified_epoch": [vp] * 8, "fm_stratified_begin": [vp] * 7,
                 "fm_stratified_step": [vp, vp, i32] + [vp] * 5, "fm_stratified_end": [vp] * 4, "fm_get_aux": [vp] * 6,
                 "fm_profile_read": [vp] * 3, "fm_destroy": [vp],
-                "fm_field_create": [i64, i32, i64, i32, vp], "fm_field_destroy": [vp],
+                "fm_field_create": [i64, i32, i64, i32, i32, vp], "fm_field_destroy": [vp],
                 "fm_field_logprobs": [vp, vp, i64, vp, i64, i32] + [vp] * 4 + [i32] + [vp] * 3,
                 "fm_field_distill": [vp, vp, i64, vp, i64, i32] + [vp] * 8}.items():
             getattr(lib, name).argtypes = types
@@ -357,9 +357,10 @@ def _out(t, n, dtype, what):
 
 class Field:
     """Owner of an ``fm_field`` handle: the C candidates of a field with K latent values each, for calls of up to
-    ``max_rows`` rows that ask for up to ``max_top`` best candidates."""
+    ``max_rows`` rows that ask for up to ``max_top`` best candidates and have up to ``max_entries`` teacher entries each
+    (0: no distillation, and no workspace for it)."""
 
-    def __init__(self, C, K, max_rows, max_top=0):
+    def __init__(self, C, K, max_rows, max_top=0, max_entries=128):
         import torch
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU: the operators of a field only run on the HIP library")
@@ -367,7 +368,7 @@ class Field:
         self.C, self.K = int(C), int(K)
         torch.cuda.current_stream()  # the runtime's device is torch's from here on
         self._h = ctypes.c_void_p(None)
-        rc = lib.fm_field_create(self.C, self.K, int(max_rows), int(max_top), ctypes.byref(self._h))
+        rc = lib.fm_field_create(self.C, self.K, int(max_rows), int(max_top), int(max_entries), ctypes.byref(self._h))
         if rc != FM_OK:
             raise FMError(rc, (lib.fm_field_last_error(None) or b"").decode())
 

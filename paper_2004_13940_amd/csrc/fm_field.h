@@ -43,7 +43,7 @@ struct FieldArgs {
     // rows against parts of the candidates
     int32_t row_tiles, splits;
     int64_t chunk;    // candidates to a split, a multiple of FM_BLOCK_CANDS
-    float4* part;     // [splits][n] FieldPart
+    float4* part;     // [splits][n] FieldPart, and the largest logit (logprobs)
     float* opart;     // [splits][n][KP] sum 2^(x - m) v_j (distillation)
     float* gmax;      // [n][blocks][4] largest logit of every group, or nullptr
     int64_t blocks;
@@ -66,8 +66,10 @@ struct FieldArgs {
     float2* rq;       // [npad] largest scaled teacher logit; S / Q, the share of the teacher in units of the exponentials
     uint4* g0;        // [npad / 16][NG][64 lanes] operands of G: 0 for rows without a part in the gradient, NaN for rows that are NaN
     uint4* gs;        // [npad / 32][KC][3][64 lanes] operands of rs G, finite
-    uint32_t* hits;   // [npad / 32][hit_words] blocks of 2^hit_shift candidates that some row of the tile names
-    int32_t hit_words, hit_shift;
+    // the teacher's entries of 32 rows by blocks of 2^entry_shift candidates: place in the block * 32 + row of the tile, share
+    uint2* entries;   // [npad / 32][32 T]
+    uint32_t* starts; // [npad / 32][entry_blocks + 1]
+    int32_t entry_blocks, entry_shift;
     int32_t col_tiles, row_splits, row_chunk;  // candidates against parts of the rows, multiples of 32 rows
     float* vpart;     // [row_splits][C][KP] parts of grad_V, and [row_splits][C] of grad_w
     float* wpart;

@@ -190,7 +190,25 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
             A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
         }
     const float4* gm = reinterpret_cast<const float4*>(A.gmax) + row * A.blocks;
-    select_best<BS>(nan ? 0 : A.blocks, A.top, best, lds, [&](int64_t q) { return gm[q]; }, [](int64_t q) { return 4 * q; });
+    // the parts of the candidates with the largest maxima, of these the groups, of these the candidates
+    const int64_t in_split = A.chunk / FM_BLOCK_CANDS;
+    int nsplits = A.splits;
+    const bool all = nsplits <= 2 * A.top;
+    if (!all && !nan) {
+        select_best<BS>((A.splits + 3) / 4, A.top, best, lds, [&](int64_t q) {
+            const auto at = [&](int64_t i) { return i < A.splits ? A.part[i * A.n + row].w : -INFINITY; };
+            return make_float4(at(4 * q), at(4 * q + 1), at(4 * q + 2), at(4 * q + 3));
+        }, [](int64_t q) { return 4 * q; });
+        nsplits = 0;
+        for (int a = 0; a < A.top; ++a) nsplits += best[a] != 0;
+        if (tid < nsplits) groups[tid] = (int32_t)key_id(best[tid]);
+        __syncthreads();
+    }
+    const auto block_of = [&](int64_t q) { return (all ? q / in_split : groups[q / in_split]) * in_split + q % in_split; };
+    select_best<BS>(nan ? 0 : nsplits * in_split, A.top, best, lds, [&](int64_t q) {
+        const int64_t at = block_of(q);
+        return at < A.blocks ? gm[at] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    }, [&](int64_t q) { return 4 * block_of(q); });
     for (int i = tid; i < 4 * A.top; i += BS) {
         const uint64_t k = best[i / 4];
         if (k == 0) continue;
@@ -229,10 +247,11 @@ template <typename TV, int KC, int BS>
 __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
 {
     constexpr int KP = 16 * KC;
-    extern __shared__ float2 entries[];  // [T] logit and scaled teacher logit, then the share of the entry
+    extern __shared__ float2 entries[];  // [T] logit and scaled teacher logit, then the share of the entry; behind them [splits] floats
     __shared__ __align__(16) float g[256];
     __shared__ FieldPart parts[BS / 64];
     __shared__ float sums[BS / 64], wide[BS];
+    float* factor = reinterpret_cast<float*>(entries + A.T);
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     // the row's part of the operands: k0..k0 + 3 of G as the logits take it, and of rs G
@@ -311,10 +330,6 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
             q = __builtin_amdgcn_exp2f(y) / Q;
             const float d = (y - log2Q) - (fmaf(e.x, A.sl, -p.m) - log2S);
             if (q != 0.f) x += q * d * FM_LN2;
-            if (counts) {
-                const int64_t at = ids[t] >> A.hit_shift;
-                atomicOr(A.hits + row / 32 * A.hit_words + (at >> 5), 1u << (at & 31));
-            }
         }
         entries[t] = make_float2(q * r, 0.f);
     }
@@ -337,6 +352,10 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
         lay_out(k, v, y);
     }
     if (A.grad_G == nullptr) return;
+    for (int i = tid; i < A.splits; i += BS) {
+        const float4 q = A.part[(int64_t)i * A.n + row];
+        factor[i] = q.y != 0.f ? __builtin_amdgcn_exp2f(q.x - p.m) : 0.f;
+    }
     __syncthreads();
     // sum over the parts of the candidates, then the teacher's share: thread = (slice of the terms, k)
     const int width = KP < BS ? KP : BS, slices = BS / width;
@@ -344,11 +363,9 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
         const int k = k0 + tid % width, slice = tid / width;
         float s = 0.f;
         if (counts) {
-            for (int i = slice; i < A.splits; i += slices) {
-                const int64_t at = (int64_t)i * A.n + row;
-                const float4 q = A.part[at];
-                if (q.y != 0.f) s = fmaf(__builtin_amdgcn_exp2f(q.x - p.m), A.opart[at * KP + k], s);
-            }
+            const float* o = A.opart + row * KP + k;
+#pragma unroll 8
+            for (int i = slice; i < A.splits; i += slices) s = fmaf(factor[i], o[(int64_t)i * A.n * KP], s);
             s *= rs;
             for (int t = slice; t < A.T; t += slices) {
                 const float q = entries[t].x;
@@ -365,18 +382,67 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
     }
 }
 
+// Lists of the teacher's entries of 32 rows by blocks of candidates.  Order inside a block does not matter: every entry has a
+// place of its own in the tile of the candidates' kernel.
+__global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
+{
+    extern __shared__ uint32_t place[];  // [entry_blocks]
+    __shared__ uint32_t sums[FM_BLOCK];
+    const int tid = threadIdx.x, i0 = blockIdx.x * 32, nb = A.entry_blocks;
+    for (int i = tid; i < nb; i += FM_BLOCK) place[i] = 0;
+    __syncthreads();
+    const auto each = [&](auto take) {
+        for (uint32_t i = tid; i < 32u * A.T; i += FM_BLOCK) {
+            const uint32_t r = i / (uint32_t)A.T;
+            if (i0 + (int)r >= A.n) break;
+            const int64_t j = A.ids[(int64_t)i0 * A.T + i];
+            if (j < 0 || j >= A.C) continue;
+            const float2 q = A.rq[i0 + r];
+            if (q.y != 0.f) take(r, j, q, i);
+        }
+    };
+    each([&](uint32_t, int64_t j, float2, uint32_t) { atomicAdd(&place[j >> A.entry_shift], 1u); });
+    __syncthreads();
+    const int per = (nb + FM_BLOCK - 1) / FM_BLOCK, first = min(tid * per, nb), last = min(first + per, nb);
+    uint32_t sum = 0;
+    for (int i = first; i < last; ++i) sum += place[i];
+    sums[tid] = sum;
+    __syncthreads();
+    for (int d = 1; d < FM_BLOCK; d *= 2) {
+        const uint32_t before = tid >= d ? sums[tid - d] : 0;
+        __syncthreads();
+        sums[tid] += before;
+        __syncthreads();
+    }
+    uint32_t at = sums[tid] - sum;
+    uint32_t* starts = A.starts + (int64_t)blockIdx.x * (nb + 1);
+    for (int i = first; i < last; ++i) {
+        const uint32_t c = place[i];
+        place[i] = starts[i] = at;
+        at += c;
+    }
+    if (tid == FM_BLOCK - 1) starts[nb] = at;
+    __syncthreads();
+    each([&](uint32_t r, int64_t j, float2 q, uint32_t i) {
+        const float share = __builtin_amdgcn_exp2f(A.teacher[(int64_t)i0 * A.T + i] * A.sl - q.x) * q.y;
+        const uint32_t in_block = (uint32_t)(j & ((int64_t(1) << A.entry_shift) - 1));
+        A.entries[(int64_t)i0 * A.T + atomicAdd(&place[j >> A.entry_shift], 1u)] = make_uint2(in_block << 5 | r, __float_as_uint(share));
+    });
+}
+
 constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most and if there is as much to do
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
-constexpr int64_t FIELD_FEW_ROWS = 256;                  // up to so many rows get a workgroup of 1024 threads, others a wavefront
+constexpr int64_t FIELD_WIDE_ROWS = 8192;                // below, a row gets a workgroup of four wavefronts, else one
 constexpr int FIELD_MOST_ENTRIES = 4096;                 // of a teacher, to a row
-constexpr int FIELD_HIT_WORDS = 512;                     // words of bits to a tile of rows, at most
+constexpr int64_t FIELD_STARTS = int64_t(1) << 26;       // starts of blocks in the lists of entries, about
+constexpr int FIELD_ENTRY_BLOCKS = 4096;                 // blocks to a list, at most
 
 }  // namespace
 
 struct fm_field {
     int64_t C, max_rows;
-    int32_t K, max_top;
+    int32_t K, max_top, max_entries;
     int device;
     bool packs;        // whether there is room for the packed table
     char* block;       // the workspace
@@ -404,18 +470,18 @@ size_t room(int64_t bytes) { return (size_t)up(bytes, 256) * 256; }
 
 int64_t whole32(int64_t n) { return up(n, 32) * 32; }
 
-// Blocks of 64 candidates or more, so many that their bits fit FIELD_HIT_WORDS.
-int32_t hit_shift(int64_t C)
+// Blocks of 2^entry_shift >= 64 candidates for the lists of entries.
+int32_t entry_shift(int64_t C, int64_t rows)
 {
     int32_t s = 6;
-    while (up(C, int64_t(1) << s) > 32 * FIELD_HIT_WORDS) ++s;
+    const int64_t tiles = std::max<int64_t>(1, whole32(rows) / 32);
+    while (up(C, int64_t(1) << s) > std::max<int64_t>(1, std::min<int64_t>(FIELD_ENTRY_BLOCKS, FIELD_STARTS / tiles))) ++s;
     return s;
 }
-int32_t hit_words(int64_t C) { return (int32_t)up(up(C, int64_t(1) << hit_shift(C)), 32); }
 
 // Where the pieces of the workspace begin.  The maxima of groups (logprobs) and what distillation needs share their place.
 struct Layout {
-    size_t part, gmax, opart, rm, rs, rq, g0, gs, hits, wpart, vpart, pv, pt, pw, bytes;
+    size_t part, gmax, opart, rm, rs, rq, g0, gs, entries, starts, wpart, vpart, pv, pt, pw, bytes;
     explicit Layout(const fm_field* f)
     {
         size_t at = 0;
@@ -424,23 +490,25 @@ struct Layout {
             at += room(bytes);
             return here;
         };
-        const int64_t KC = fm_field_chunks(f->K), KP = 16 * KC, rows = whole32(f->max_rows), cands = up(f->C, FM_BLOCK_CANDS) * FM_BLOCK_CANDS;
+        const bool distill = f->max_entries > 0, packed = f->packs;
+        const int64_t KC = fm_field_chunks(f->K), KP = 16 * KC, rows = distill ? whole32(f->max_rows) : 0;
+        const int64_t cands = up(f->C, FM_BLOCK_CANDS) * FM_BLOCK_CANDS;
         part = take(f->slots * 16);
-        const bool packed = f->packs;
         pv = take(packed ? cands / 16 * 1024 * (KC == 1 ? 2 : 3 * KC / 2) : 0);
         pw = take(packed ? cands * 4 : 0);
         gmax = opart = at;
         const size_t top = at + room(f->top_rows * up(f->C, FM_BLOCK_CANDS) * 16);
-        take(f->slots * KP * 4);
+        take(distill ? f->slots * KP * 4 : 0);
         rm = take(rows * 4);
         rs = take(rows * 4);
         rq = take(rows * 8);
         g0 = take(rows / 16 * 1024 * (KC == 1 ? 3 : 3 * KC / 2));
         gs = take(rows / 32 * 1024 * 3 * KC);
-        hits = take(rows / 32 * hit_words(f->C) * 4);
+        entries = take(rows * f->max_entries * 8);
+        starts = take(rows / 32 * (up(f->C, int64_t(1) << entry_shift(f->C, f->max_rows)) + 1) * 4);
         wpart = take(f->col_parts * 4);
         vpart = take(f->col_parts * KP * 4);
-        pt = take(packed ? cands / 32 * 1024 * 3 * KC : 0);
+        pt = take(packed && distill ? cands / 32 * 1024 * 3 * KC : 0);
         bytes = std::max(at, top);
     }
 };
@@ -505,12 +573,13 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.pv = reinterpret_cast<uint4*>(f->block + at.pv);
     A.pt = reinterpret_cast<uint4*>(f->block + at.pt);
     A.pw = floats(at.pw);
-    A.hits = reinterpret_cast<uint32_t*>(f->block + at.hits);
+    A.entries = reinterpret_cast<uint2*>(f->block + at.entries);
+    A.starts = reinterpret_cast<uint32_t*>(f->block + at.starts);
     A.wpart = floats(at.wpart);
     A.vpart = floats(at.vpart);
     A.npad = (int32_t)whole32(n);
-    A.hit_shift = hit_shift(f->C);
-    A.hit_words = hit_words(f->C);
+    A.entry_shift = entry_shift(f->C, f->max_rows);
+    A.entry_blocks = (int32_t)up(f->C, int64_t(1) << A.entry_shift);
     A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
     const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 32));
     A.row_chunk = (int32_t)std::max<int64_t>(32, up(up(A.npad, parts), 32) * 32);
@@ -538,7 +607,7 @@ void by_type(int32_t type, F run)
 
 extern "C" const char* fm_field_last_error(const fm_field* f) { return f != nullptr ? f->err : g_create_error; }
 
-extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t max_top, fm_field** out)
+extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t max_top, int32_t max_entries, fm_field** out)
 {
     if (out == nullptr) return fail(nullptr, FM_EINVAL, "out must not be NULL");
     *out = nullptr;
@@ -547,18 +616,21 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     if (C < 1 || C > INT32_MAX || max_rows < 1 || max_rows > INT32_MAX)
         return fail(nullptr, FM_ERANGE, "C=%lld and max_rows=%lld must be 1..2^31-1", (long long)C, (long long)max_rows);
     if (max_top < 0 || max_top > FM_FIELD_TOP) return fail(nullptr, FM_ERANGE, "max_top=%d outside 0..%d", max_top, FM_FIELD_TOP);
+    if (max_entries < 0 || max_entries > FIELD_MOST_ENTRIES)
+        return fail(nullptr, FM_ERANGE, "max_entries=%d outside 0..%d", max_entries, FIELD_MOST_ENTRIES);
     fm_field* f = new (std::nothrow) fm_field();
     if (f == nullptr) return fail(nullptr, FM_ENOMEM, "no host memory");
     f->C = C;
     f->K = K;
     f->max_rows = max_rows;
     f->max_top = max_top;
-    f->packs = max_rows > FIELD_DIRECT_ROWS && fm_field_pack_bytes(true, K, C) <= FIELD_PACK_BYTES;
+    f->max_entries = max_entries;
+    f->packs = max_rows > FIELD_DIRECT_ROWS && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
     // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
     f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
     const int64_t tiles = up(C, fm_field_cols_per_wave(K));
     const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole32(max_rows) / 32);
-    f->col_parts = col_parts > 1 ? C * col_parts : 0;  // a single part is written to where it belongs
+    f->col_parts = col_parts > 1 && max_entries > 0 ? C * col_parts : 0;  // a single part is written to where it belongs
     f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / (4 * up(C, FM_BLOCK_CANDS))));
     const size_t bytes = Layout(f).bytes;
     hipError_t e = hipGetDevice(&f->device);
@@ -614,9 +686,9 @@ extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n,
             using TV = std::remove_pointer_t<decltype(t)>;
             const uint32_t rows = (uint32_t)A.n, lds = (uint32_t)top * 4 * 16 * sizeof(float);
             if (top == 0)
-                n <= FIELD_FEW_ROWS ? k_field_finish<TV, 1024><<<rows, 1024, 0, st>>>(A) : k_field_finish<TV, 64><<<rows, 64, 0, st>>>(A);
+                n < FIELD_WIDE_ROWS ? k_field_finish<TV, FM_BLOCK><<<rows, FM_BLOCK, 0, st>>>(A) : k_field_finish<TV, 64><<<rows, 64, 0, st>>>(A);
             else
-                n <= FIELD_FEW_ROWS ? k_field_finish_top<TV, 1024><<<rows, 1024, lds, st>>>(A) : k_field_finish_top<TV, 64><<<rows, 64, lds, st>>>(A);
+                n < FIELD_WIDE_ROWS ? k_field_finish_top<TV, FM_BLOCK><<<rows, FM_BLOCK, lds, st>>>(A) : k_field_finish_top<TV, 64><<<rows, 64, lds, st>>>(A);
         });
         FM_TRY(launched(f));
     }
@@ -629,7 +701,7 @@ extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, 
 {
     if (f == nullptr) return FM_EINVAL;
     FM_TRY(check(f, c, n, G, g_stride));
-    if (T > FIELD_MOST_ENTRIES) return fail(f, FM_ERANGE, "T=%d: at most %d entries to a row", T, FIELD_MOST_ENTRIES);
+    if (T > f->max_entries) return fail(f, FM_ERANGE, "T=%d: the handle was made for at most %d entries to a row", T, f->max_entries);
     if (T < 1 || (n > 0 && (ids == nullptr || teacher == nullptr))) return fail(f, FM_EINVAL, "ids and teacher of T=%d >= 1 entries to a row are needed", T);
     hipStream_t st = (hipStream_t)hip_stream;
     if (n > FIELD_MOST_ROWS) return fail(f, FM_ERANGE, "n=%lld: at most %lld rows to a call", (long long)n, (long long)FIELD_MOST_ROWS);
@@ -647,10 +719,12 @@ extern "C" int fm_field_distill(fm_field* f, const fm_candidates* c, int64_t n, 
         fm_field_shape(c->v_type, f->K, [&](auto type, auto kc, auto) {
             using TV = decltype(type);
             constexpr int KC = decltype(kc)::value;
-            const uint32_t rows = (uint32_t)A.npad, lds = (uint32_t)T * sizeof(float2);
-            n <= FIELD_FEW_ROWS ? k_field_distill_rows<TV, KC, 1024><<<rows, 1024, lds, st>>>(A)
+            const uint32_t rows = (uint32_t)A.npad, lds = (uint32_t)(T * sizeof(float2) + A.splits * sizeof(float));
+            n < FIELD_WIDE_ROWS ? k_field_distill_rows<TV, KC, FM_BLOCK><<<rows, FM_BLOCK, lds, st>>>(A)
                                 : k_field_distill_rows<TV, KC, 64><<<rows, 64, lds, st>>>(A);
         });
+        if (grad_V != nullptr || grad_w != nullptr)
+            k_field_entries<<<A.npad / 32, FM_BLOCK, (size_t)A.entry_blocks * sizeof(uint32_t), st>>>(A);
     }
     if (grad_V != nullptr || grad_w != nullptr) fm_field_cols(c->v_type, A, st);
     return launched(f);

@@ -14,7 +14,7 @@ __device__ __forceinline__ void wave_sync()
 // A wavefront takes 16 NT candidates and a part of the rows, 32 of them at a time.  The tiles of logits have rows down and
 // candidates across, so that they are the B operand of the second product (rows are what it sums over) as they stand:
 //   grad_V^T[k][j] += gs[i][k] P[i][j],   P_ij = 2^(x_ij - m_i) - (share of the teacher),   gs = weight scale / S G.
-// The teacher's few entries come into the tile by way of LDS, in tiles that have a bit set for their block of candidates.
+// The teacher's few entries come into the tiles by way of LDS.
 template <typename TV, int KC, int FILL, int NT>
 __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
 {
@@ -54,8 +54,8 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
         Ops::of_v(p, b[t]);
     }
     const bool row_masks = A.mask != nullptr && A.mask_stride != 0;
-    const uint32_t* hits = A.hits + (c0 >> A.hit_shift >> 5);
-    const uint32_t hit = 1u << (c0 >> A.hit_shift & 31);
+    const uint32_t* starts = A.starts + (c0 >> A.entry_shift);
+    const uint32_t in_block = (uint32_t)(c0 & ((int64_t(1) << A.entry_shift) - 1));
 
     for (int i0 = beg; i0 < end; i0 += 32) {
         f32x4 z[2][NT], m[2], rs[2];
@@ -83,15 +83,14 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
                 }
         }
         const auto exponential = [&](int h, int t, int r) { return __builtin_amdgcn_exp2f(fmaf(z[h][t][r], A.sl, -m[h][r])); };
-        if (hits[(int64_t)(i0 / 32) * A.hit_words] & hit) {  // the same in all lanes
-            for (int i = lane; i < 32 * A.T; i += 64) {
-                const int row = i0 + i / A.T;
-                if (row >= A.n) break;
-                const int64_t j = A.ids[(int64_t)row * A.T + i % A.T] - c0;
-                if (j < 0 || j >= 16 * NT || c0 + j >= A.C) continue;
-                const float2 q = A.rq[row];
-                const float share = __builtin_amdgcn_exp2f(A.teacher[(int64_t)row * A.T + i % A.T] * A.sl - q.x) * q.y;
-                atomicAdd(&Q[j * QS + i / A.T], share);  // into zero but for ids that come twice
+        const uint32_t* range = starts + (int64_t)(i0 / 32) * (A.entry_blocks + 1);
+        const uint32_t from = range[0], to = range[1];  // the same in all lanes
+        if (from != to) {
+            const uint2* entries = A.entries + (int64_t)i0 * A.T;
+            for (uint32_t i = from + lane; i < to; i += 64) {
+                const uint2 e = entries[i];
+                const uint32_t j = (e.x >> 5) - in_block;
+                if (j < 16 * NT) atomicAdd(&Q[j * QS + (e.x & 31)], __uint_as_float(e.y));  // into zero but for ids that come twice
             }
             wave_sync();
 #pragma unroll

@@ -9,7 +9,7 @@ namespace {
 // sums o of the candidates, of which the four lanes of a row hold the latent values 16 c + 4 g + r.
 template <int KC, int NT, bool DISTILL>
 struct RowStats {
-    float m[NT], S[NT], U[NT];
+    float m[NT], S[NT], U[NT], best[NT];
     f32x4 o[DISTILL ? KC : 1][NT];
 
     __device__ __forceinline__ RowStats()
@@ -18,6 +18,7 @@ struct RowStats {
         for (int t = 0; t < NT; ++t) {
             m[t] = -3e38f;
             S[t] = U[t] = 0.f;
+            best[t] = -INFINITY;
 #pragma unroll
             for (int c = 0; c < (DISTILL ? KC : 1); ++c) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -37,6 +38,7 @@ struct RowStats {
             x = fmaxf(fmaxf(x, z[2][t][3]), z[3][t][0]);
             x = fmaxf(fmaxf(x, z[3][t][1]), z[3][t][2]);
             top[t] = fmaxf(x, z[3][t][3]);
+            if constexpr (!DISTILL) best[t] = fmaxf(best[t], top[t]);
             rise |= top[t] * sl > m[t] + 8.f;
         }
         if (!__any(rise)) return;
@@ -79,9 +81,14 @@ struct RowStats {
             FieldPart p = {m[t], S[t], U[t]};
             p = fm_field_merge(p, {fm_xor_lane<16>(p.m), fm_xor_lane<16>(p.S), fm_xor_lane<16>(p.U)});
             p = fm_field_merge(p, {fm_xor_lane<32>(p.m), fm_xor_lane<32>(p.S), fm_xor_lane<32>(p.U)});
+            float most = 0.f;
+            if constexpr (!DISTILL) {
+                most = fmaxf(best[t], fm_xor_lane<16>(best[t]));
+                most = fmaxf(most, fm_xor_lane<32>(most));
+            }
             if (row >= A.n) continue;
             const int64_t at = (int64_t)split * A.n + row;
-            if (g == 0) A.part[at] = make_float4(p.m, p.S, p.U, 0.f);
+            if (g == 0) A.part[at] = make_float4(p.m, p.S, p.U, most);
             if constexpr (DISTILL)
 #pragma unroll
                 for (int c = 0; c < KC; ++c) *reinterpret_cast<f32x4*>(A.opart + at * 16 * KC + 16 * c + 4 * g) = o[c][t];
@@ -111,13 +118,6 @@ __device__ __forceinline__ void store_maxima(const FieldArgs& A, const float (&t
     }
 }
 
-// Bits that k_field_distill_rows sets.
-__device__ __forceinline__ void clear_hits(const FieldArgs& A)
-{
-    const int64_t words = (int64_t)(A.npad / 32) * A.hit_words;
-    for (int64_t i = (int64_t)blockIdx.x * FM_BLOCK + threadIdx.x; i < words; i += (int64_t)gridDim.x * FM_BLOCK) A.hits[i] = 0;
-}
-
 // A wavefront takes 16 NT rows and a part of the candidates, 16 of them at a time.  The tile of logits has candidates down
 // and rows across, so that a lane has four candidates of one row of every 16: maxima and sums stay in the lane, and the tile
 // is the B operand of the second product (candidates are what it sums over) as it stands.  fp32 products straight from V:
@@ -128,7 +128,6 @@ __global__ __launch_bounds__(FM_BLOCK, KC == 16 ? 1 : 2) void k_field_rows(const
     constexpr int KP = 16 * KC;
     const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
     const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if constexpr (DISTILL) clear_hits(A);
     if (item >= (int64_t)A.row_tiles * A.splits) return;
     const int split = (int)(item / A.row_tiles), row0 = (int)(item % A.row_tiles) * 16 * NT;
     const int64_t beg = split * A.chunk, end = min(A.C, beg + A.chunk);
@@ -271,7 +270,6 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldAr
     using Ops = FieldOps<NP, KC>;
     const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
     const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if constexpr (DISTILL) clear_hits(A);
     if (item >= (int64_t)A.row_tiles * A.splits) return;
     const int split_no = (int)(item / A.row_tiles), row0 = (int)(item % A.row_tiles) * 16 * NT;
     const int64_t beg = split_no * A.chunk, end = min(A.C, beg + A.chunk);
