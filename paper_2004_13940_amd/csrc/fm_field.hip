@@ -48,11 +48,10 @@ __device__ __forceinline__ uint64_t item_key(float z, int64_t id)
 }
 __device__ __forceinline__ int64_t key_id(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 
-// The `top` largest keys of 4 * quads items into best[0..top), in order, 0 from where there are no more.  values(q) are the
-// values of items 4 q..4 q + 3, number(q) is the number of the first of them.  Items go to 64 buckets; what is below the
-// top-th largest of the buckets' maxima is not among the best, and of what is not (a few more than `top` if the order of the items has
-// nothing to do with the buckets), everyone counts who is before it.  Where that is more than the list holds, the best are
-// taken one by one.  Ends with a barrier.
+// The `top` largest keys of `count` items into best[0..top), in order, 0 from where there are no more; item i has value(i) and
+// number(i).  Items go to 64 buckets: what is below the top-th largest of the buckets' maxima is not among the best, and of
+// what is not (a few more than `top`, if the order of the items has nothing to do with the buckets) everyone counts who is
+// before it.  Where that is more than the list holds, the top-th of those in the list is the next bound.  Ends with a barrier.
 constexpr int SELECT_LIST = 512;
 template <int BS>
 struct SelectLds {
@@ -61,24 +60,15 @@ struct SelectLds {
 };
 
 template <int BS, typename F, typename N>
-__device__ __forceinline__ void select_best(int64_t quads, int top, uint64_t* best, SelectLds<BS>& lds, F values, N number)
+__device__ __forceinline__ void select_best(int64_t count, int top, uint64_t* best, SelectLds<BS>& lds, F value, N number)
 {
     const int tid = threadIdx.x;
-    const auto each = [&](auto take) {
-        for (int64_t q = tid; q < quads; q += BS) {
-            const float4 v = values(q);
-            const int64_t id = number(q);
-            take(v.x, id);
-            take(v.y, id + 1);
-            take(v.z, id + 2);
-            take(v.w, id + 3);
-        }
-    };
     uint64_t mine = 0;
-    each([&](float z, int64_t id) {
-        const uint64_t k = item_key(z, id);
+#pragma unroll 4
+    for (int64_t i = tid; i < count; i += BS) {
+        const uint64_t k = item_key(value(i), number(i));
         mine = k > mine ? k : mine;
-    });
+    }
     lds.max[tid] = mine;
     if (tid == 0) lds.count = 0, lds.from = 1;
     for (int a = tid; a < top; a += BS) best[a] = 0;
@@ -94,41 +84,31 @@ __device__ __forceinline__ void select_best(int64_t quads, int top, uint64_t* be
         for (int i = 0; i < 64; ++i) before += lds.list[i] > mine;
         if (mine != 0 && before == top - 1) lds.from = mine;
     }
-    __syncthreads();
-    const uint64_t from = lds.from;
-    each([&](float z, int64_t id) {
-        const uint64_t k = item_key(z, id);
-        if (k >= from) {
-            const int at = atomicAdd(&lds.count, 1);
-            if (at < SELECT_LIST) lds.list[at] = k;
+    for (;;) {
+        __syncthreads();
+        const uint64_t from = lds.from;
+#pragma unroll 4
+        for (int64_t i = tid; i < count; i += BS) {
+            const uint64_t k = item_key(value(i), number(i));
+            if (k >= from) {
+                const int at = atomicAdd(&lds.count, 1);
+                if (at < SELECT_LIST) lds.list[at] = k;
+            }
         }
-    });
-    __syncthreads();
-    const int count = lds.count;
-    if (count <= SELECT_LIST) {
-        for (int i = tid; i < count; i += BS) {
+        __syncthreads();
+        const int found = lds.count, held = min(found, SELECT_LIST);
+        for (int i = tid; i < held; i += BS) {
             const uint64_t k = lds.list[i];
             int before = 0;
-            for (int o = 0; o < count; ++o) before += lds.list[o] > k;
+#pragma unroll 4
+            for (int o = 0; o < held; ++o) before += lds.list[o] > k;
             if (before < top) best[before] = k;
+            if (before == top - 1) lds.from = k;
         }
-    } else {
-        uint64_t below = ~0ull;
-        for (int a = 0; a < top && below != 0; ++a) {
-            mine = 0;
-            each([&](float z, int64_t id) {
-                const uint64_t k = item_key(z, id);
-                mine = k < below && k > mine ? k : mine;
-            });
-            lds.max[tid] = mine;
-            __syncthreads();
-            for (int i = 0; i < BS; ++i) mine = lds.max[i] > mine ? lds.max[i] : mine;
-            __syncthreads();
-            below = mine;
-            if (tid == 0) best[a] = mine;
-        }
+        __syncthreads();
+        if (found <= SELECT_LIST) return;
+        if (tid == 0) lds.count = 0;
     }
-    __syncthreads();
 }
 
 // What is left of a row: its sums joined, given candidates, best candidates.
@@ -189,51 +169,52 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
             const int64_t j = A.ids[row * A.T + t];
             A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
         }
-    const float4* gm = reinterpret_cast<const float4*>(A.gmax) + row * A.blocks;
-    // the parts of the candidates with the largest maxima, of these the groups, of these the candidates
-    const int64_t in_split = A.chunk / FM_BLOCK_CANDS;
-    int nsplits = A.splits;
-    const bool all = nsplits <= 2 * A.top;
-    if (!all && !nan) {
-        select_best<BS>((A.splits + 3) / 4, A.top, best, lds, [&](int64_t q) {
-            const auto at = [&](int64_t i) { return i < A.splits ? A.part[i * A.n + row].w : -INFINITY; };
-            return make_float4(at(4 * q), at(4 * q + 1), at(4 * q + 2), at(4 * q + 3));
-        }, [](int64_t q) { return 4 * q; });
-        nsplits = 0;
-        for (int a = 0; a < A.top; ++a) nsplits += best[a] != 0;
-        if (tid < nsplits) groups[tid] = (int32_t)key_id(best[tid]);
+    // of the parts of the candidates those with the largest maxima, of these the groups, of these the candidates
+    const float* gm = A.gmax + row * A.blocks * 4;
+    const int64_t in_split = A.chunk / FM_BLOCK_CANDS * 4;  // groups
+    const bool all = A.splits <= 2 * A.top || A.splits * in_split <= 4 * BS;
+    int nsplits = A.splits, ng = 0;
+    const auto group = [&](int64_t i) {  // i-th group of the parts that were taken
+        return all ? i : groups[(int)(i / in_split)] * in_split + i % in_split;
+    };
+    const auto candidate = [&](int64_t i) {  // i-th candidate of the groups that were taken
+        const int64_t id = groups[i / 16];
+        return id / 4 * FM_BLOCK_CANDS + 4 * (id % 4) + i % 16 / 4 * 16 + i % 4;
+    };
+    for (int stage = all ? 1 : 0; stage < 3; ++stage) {
+        const int64_t count = nan ? 0 : stage == 0 ? A.splits : stage == 1 ? nsplits * in_split : 16 * ng;
+        select_best<BS>(count, A.top, best, lds, [&](int64_t i) {
+            if (stage == 0) return A.part[i * A.n + row].w;
+            if (stage == 2) return zs[i];
+            const int64_t at = group(i);
+            return at < A.blocks * 4 ? gm[at] : -INFINITY;
+        }, [&](int64_t i) { return stage == 0 ? i : stage == 1 ? group(i) : candidate(i); });
+        if (stage == 0) {
+            nsplits = 0;
+            for (int a = 0; a < A.top; ++a) nsplits += best[a] != 0;
+            if (tid < nsplits) groups[tid] = (int32_t)key_id(best[tid]);
+        } else if (stage == 1) {
+            for (int i = tid; i < 4 * A.top; i += BS) {
+                const uint64_t k = best[i / 4];
+                if (k == 0) continue;
+                const int64_t id = key_id(k), other = id / 4 * 4 + i % 4;
+                bool take = other == id;
+                if (!take) {  // equal to the last one that was taken, and not taken itself
+                    const uint64_t last = best[A.top - 1], mine = item_key(gm[other], other);
+                    take = last != 0 && mine < last && mine >> 32 == last >> 32;
+                    for (int o = 0; take && o < i / 4; ++o) take = best[o] == 0 || key_id(best[o]) / 4 != id / 4;  // once for the block
+                }
+                if (take) groups[atomicAdd(&ngroups, 1)] = (int32_t)other;
+            }
+            __syncthreads();
+            ng = ngroups;
+            for (int i = tid; i < 16 * ng; i += BS) {
+                const int64_t j = candidate(i);
+                zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
+            }
+        }
         __syncthreads();
     }
-    const auto block_of = [&](int64_t q) { return (all ? q / in_split : groups[q / in_split]) * in_split + q % in_split; };
-    select_best<BS>(nan ? 0 : nsplits * in_split, A.top, best, lds, [&](int64_t q) {
-        const int64_t at = block_of(q);
-        return at < A.blocks ? gm[at] : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    }, [&](int64_t q) { return 4 * block_of(q); });
-    for (int i = tid; i < 4 * A.top; i += BS) {
-        const uint64_t k = best[i / 4];
-        if (k == 0) continue;
-        const int64_t id = key_id(k), other = id / 4 * 4 + i % 4;
-        bool take = other == id;
-        if (!take) {  // equal to the last one that was taken, and not taken itself
-            const float4 v = gm[id / 4];
-            const uint64_t last = best[A.top - 1], mine = item_key(i % 4 == 0 ? v.x : i % 4 == 1 ? v.y : i % 4 == 2 ? v.z : v.w, other);
-            take = last != 0 && mine < last && mine >> 32 == last >> 32;
-            for (int o = 0; take && o < i / 4; ++o) take = best[o] == 0 || key_id(best[o]) / 4 != id / 4;  // once for the block
-        }
-        if (take) groups[atomicAdd(&ngroups, 1)] = (int32_t)other;
-    }
-    __syncthreads();
-    const int ng = ngroups;
-    const auto first = [&](int64_t q) {  // of four consecutive candidates: 16 i of group q / 4
-        const int64_t id = groups[q / 4];
-        return id / 4 * FM_BLOCK_CANDS + 16 * (q % 4) + 4 * (id % 4);
-    };
-    for (int i = tid; i < 16 * ng; i += BS) {
-        const int64_t j = first(i / 4) + i % 4;
-        zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
-    }
-    __syncthreads();
-    select_best<BS>(4 * ng, A.top, best, lds, [&](int64_t q) { return reinterpret_cast<const float4*>(zs)[q]; }, first);
     for (int a = tid; a < A.top; a += BS) {
         const uint64_t k = best[a];
         if (A.top_ids != nullptr) A.top_ids[row * A.top + a] = k == 0 ? -1 : (int32_t)key_id(k);
@@ -433,7 +414,7 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
 constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most and if there is as much to do
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
-constexpr int64_t FIELD_WIDE_ROWS = 8192;                // below, a row gets a workgroup of four wavefronts, else one
+constexpr int64_t FIELD_WIDE_ROWS = 2048;                // below, a row gets a workgroup of four wavefronts, else one
 constexpr int FIELD_MOST_ENTRIES = 4096;                 // of a teacher, to a row
 constexpr int64_t FIELD_STARTS = int64_t(1) << 26;       // starts of blocks in the lists of entries, about
 constexpr int FIELD_ENTRY_BLOCKS = 4096;                 // blocks to a list, at most
@@ -556,8 +537,10 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.packed = f->packs && n > FIELD_DIRECT_ROWS;
     const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed);
     A.row_tiles = (int32_t)up(n, per);
-    const int64_t splits = std::max<int64_t>(1, std::min(FIELD_ITEMS / std::max(A.row_tiles, 1), (int32_t)std::min<int64_t>(up(f->C, FM_BLOCK_CANDS), INT32_MAX)));
-    A.chunk = up(up(f->C, splits), FM_BLOCK_CANDS) * FM_BLOCK_CANDS;
+    // straight from V a part of the candidates is shared by the wavefronts of a workgroup
+    const int64_t share = A.packed ? 1 : FM_FIELD_SHARE, blocks = up(f->C, FM_BLOCK_CANDS);
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / share / std::max(A.row_tiles, 1), up(blocks, share)));
+    A.chunk = up(blocks, splits) * FM_BLOCK_CANDS;
     A.splits = (int32_t)up(f->C, A.chunk);
     A.blocks = up(f->C, FM_BLOCK_CANDS);
     const Layout at(f);

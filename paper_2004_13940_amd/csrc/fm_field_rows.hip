@@ -73,22 +73,30 @@ struct RowStats {
         }
     }
 
+    // One part of each row from its four lanes.
+    __device__ __forceinline__ void join()
+    {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            FieldPart p = {m[t], S[t], U[t]};
+            p = fm_field_merge(p, {fm_xor_lane<16>(p.m), fm_xor_lane<16>(p.S), fm_xor_lane<16>(p.U)});
+            p = fm_field_merge(p, {fm_xor_lane<32>(p.m), fm_xor_lane<32>(p.S), fm_xor_lane<32>(p.U)});
+            m[t] = p.m, S[t] = p.S, U[t] = p.U;
+            if constexpr (!DISTILL) {
+                best[t] = fmaxf(best[t], fm_xor_lane<16>(best[t]));
+                best[t] = fmaxf(best[t], fm_xor_lane<32>(best[t]));
+            }
+        }
+    }
+
     __device__ __forceinline__ void leave(const FieldArgs& A, int split, int row0, int lo, int g)
     {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int row = row0 + 16 * t + lo;
-            FieldPart p = {m[t], S[t], U[t]};
-            p = fm_field_merge(p, {fm_xor_lane<16>(p.m), fm_xor_lane<16>(p.S), fm_xor_lane<16>(p.U)});
-            p = fm_field_merge(p, {fm_xor_lane<32>(p.m), fm_xor_lane<32>(p.S), fm_xor_lane<32>(p.U)});
-            float most = 0.f;
-            if constexpr (!DISTILL) {
-                most = fmaxf(best[t], fm_xor_lane<16>(best[t]));
-                most = fmaxf(most, fm_xor_lane<32>(most));
-            }
             if (row >= A.n) continue;
             const int64_t at = (int64_t)split * A.n + row;
-            if (g == 0) A.part[at] = make_float4(p.m, p.S, p.U, most);
+            if (g == 0) A.part[at] = make_float4(m[t], S[t], U[t], best[t]);
             if constexpr (DISTILL)
 #pragma unroll
                 for (int c = 0; c < KC; ++c) *reinterpret_cast<f32x4*>(A.opart + at * 16 * KC + 16 * c + 4 * g) = o[c][t];
@@ -118,18 +126,17 @@ __device__ __forceinline__ void store_maxima(const FieldArgs& A, const float (&t
     }
 }
 
-// A wavefront takes 16 NT rows and a part of the candidates, 16 of them at a time.  The tile of logits has candidates down
-// and rows across, so that a lane has four candidates of one row of every 16: maxima and sums stay in the lane, and the tile
-// is the B operand of the second product (candidates are what it sums over) as it stands.  fp32 products straight from V:
-// for calls with so few rows that laying V out would cost more than it saves.
-template <typename TV, int KC, int FILL, int NT, bool DISTILL>
-__global__ __launch_bounds__(FM_BLOCK, KC == 16 ? 1 : 2) void k_field_rows(const FieldArgs A)
+// A wavefront takes 16 rows and a part of the candidates, 16 of them at a time.  The tile of logits has candidates down and
+// rows across, so that a lane has four candidates of one row: maxima and sums stay in the lane, and the tile is the B operand
+// of the second product (candidates are what it sums over) as it stands.  fp32 products straight from V: for calls with so
+// few rows that laying V out would cost more than it saves.  The wavefronts of a workgroup share the rows and the part.
+template <typename TV, int KC, int FILL, bool DISTILL>
+__global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldArgs A)
 {
-    constexpr int KP = 16 * KC;
+    constexpr int NT = 1, W = FM_FIELD_SHARE;
     const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
-    const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (item >= (int64_t)A.row_tiles * A.splits) return;
-    const int split = (int)(item / A.row_tiles), row0 = (int)(item % A.row_tiles) * 16 * NT;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int split = (int)blockIdx.x / A.row_tiles, row0 = (int)blockIdx.x % A.row_tiles * 16;
     const int64_t beg = split * A.chunk, end = min(A.C, beg + A.chunk);
     const TV* V = static_cast<const TV*>(A.V);
 
@@ -146,7 +153,7 @@ __global__ __launch_bounds__(FM_BLOCK, KC == 16 ? 1 : 2) void k_field_rows(const
         }
     }
     RowStats<KC, NT, DISTILL> s;
-    for (int64_t j0 = beg; j0 < end; j0 += FM_BLOCK_CANDS) {
+    for (int64_t j0 = beg + wave * FM_BLOCK_CANDS; j0 < end; j0 += W * FM_BLOCK_CANDS) {
         f32x4 z[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -205,6 +212,38 @@ __global__ __launch_bounds__(FM_BLOCK, KC == 16 ? 1 : 2) void k_field_rows(const
             }
         }
     }
+    // the wavefronts' parts: a row's four lanes have the same statistics from here on
+    __shared__ float4 parts[W][16];
+    __shared__ f32x4 sums[DISTILL ? W / 2 : 1][DISTILL ? KC : 1][64];
+    s.join();
+    if (g == 0) parts[wave][lo] = make_float4(s.m[0], s.S[0], s.U[0], s.best[0]);
+    __syncthreads();
+    const float own = s.m[0];
+    FieldPart p = {-INFINITY, 0.f, 0.f};
+    float best = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const float4 q = parts[i][lo];
+        p = fm_field_merge(p, {q.x, q.y, q.z});
+        best = fmaxf(best, q.w);
+    }
+    if constexpr (DISTILL) {
+        const float f = s.S[0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(own - p.m);
+#pragma unroll
+        for (int c = 0; c < KC; ++c) s.o[c][0] *= f;
+        for (int half = W / 2; half > 0; half /= 2) {
+            if (wave >= half && wave < 2 * half)
+#pragma unroll
+                for (int c = 0; c < KC; ++c) sums[wave - half][c][lane] = s.o[c][0];
+            __syncthreads();
+            if (wave < half)
+#pragma unroll
+                for (int c = 0; c < KC; ++c) s.o[c][0] += sums[wave][c][lane];
+            __syncthreads();
+        }
+    }
+    if (wave > 0) return;
+    s.m[0] = p.m, s.S[0] = p.S, s.U[0] = p.U, s.best[0] = best;
     s.leave(A, split, row0, lo, g);
 }
 
@@ -344,6 +383,7 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldAr
             }
         }
     }
+    s.join();
     s.leave(A, split_no, row0, lo, g);
 }
 
@@ -360,7 +400,7 @@ void rows(int32_t v_type, const FieldArgs& A, hipStream_t st)
             k_field_pack<TV, KC, FILL, DISTILL><<<blocks_of(A.blocks * 2), FM_BLOCK, 0, st>>>(A);
             k_field_rows_packed<FmParts<TV>::value, KC, fm_field_row_tiles(KC, DISTILL), DISTILL><<<grid, FM_BLOCK, 0, st>>>(A);
         } else {
-            k_field_rows<TV, KC, FILL, 1, DISTILL><<<grid, FM_BLOCK, 0, st>>>(A);
+            k_field_rows<TV, KC, FILL, DISTILL><<<(uint32_t)(A.row_tiles * A.splits), 64 * FM_FIELD_SHARE, 0, st>>>(A);
         }
     });
 }

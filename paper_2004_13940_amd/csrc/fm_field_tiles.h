@@ -135,6 +135,8 @@ constexpr int fm_field_chunks(int32_t K) { return K <= 16 ? 1 : K <= 32 ? 2 : K 
 constexpr int fm_field_row_tiles(int KC, bool distill) { return KC <= (distill ? 1 : 2) ? 4 : KC <= (distill ? 4 : 8) ? 2 : 1; }
 constexpr int fm_field_col_tiles(int KC) { return KC <= 1 ? 4 : KC <= 4 ? 2 : 1; }
 
+constexpr int FM_FIELD_SHARE = 8;  // wavefronts to a part of the candidates in calls with few rows
+
 template <int V> using IntC = std::integral_constant<int, V>;
 
 // Calls run(a value of V's type, chunks, how K fills them).
@@ -145,7 +147,9 @@ void fm_field_shape(int32_t v_type, int32_t K, F run)
         const int kc = fm_field_chunks(K);
         const auto of = [&](auto chunks) {
             if (K == 16 * kc) return run(type, chunks, IntC<FILL_WHOLE>{});
-            K % 4 == 0 ? run(type, chunks, IntC<FILL_QUADS>{}) : run(type, chunks, IntC<FILL_ANY>{});
+            if constexpr (decltype(chunks)::value < 16)  // there quads would take more registers than there are
+                if (K % 4 == 0) return run(type, chunks, IntC<FILL_QUADS>{});
+            run(type, chunks, IntC<FILL_ANY>{});
         };
         switch (kc) {
             case 1: return of(IntC<1>{});
