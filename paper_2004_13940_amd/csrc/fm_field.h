@@ -30,6 +30,8 @@ __device__ __forceinline__ FieldPart fm_field_merge(FieldPart a, FieldPart b)
     return r;
 }
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
 struct FieldArgs {
     const void* V;
     const float* w;
@@ -40,6 +42,7 @@ struct FieldArgs {
     int64_t C;
     int32_t n, K;
     float scale, sl;  // sl = scale log2(e)
+    float out;        // logit of what is left out, in place of -infinity: so low that 2^(scale out - m) is 0, and that times it too
     // rows against parts of the candidates
     int32_t row_tiles, splits;
     int64_t chunk;    // candidates to a split, a multiple of FM_BLOCK_CANDS
@@ -49,8 +52,8 @@ struct FieldArgs {
     int64_t blocks;
     // V and w laid out for the matrix cores, if there are rows enough to pay for it
     bool packed;
-    uint4* pv;        // [candidates / 16][NV][64 lanes] operands of the logits
-    uint4* pt;        // [candidates / 32][KC][NP][64 lanes] operands of the sum of candidates, finite
+    u32x4* pv;        // [candidates / 16][NV][64 lanes] operands of the logits
+    u32x4* pt;        // [candidates / 32][KC][NP][64 lanes] operands of the sum of candidates, finite
     float* pw;        // [candidates] w; -infinity for those that no row allows and beyond C
     // logprobs
     const int32_t* ids;
@@ -61,11 +64,10 @@ struct FieldArgs {
     const float *teacher, *weight;
     float *loss, *grad_G, *grad_V, *grad_w;
     int32_t npad;     // n in whole tiles of 32 rows
-    float* rm;        // [npad] reference m of the row's exponentials
-    float* rs;        // [npad] weight scale / S; 0: no part in the gradient
+    float* rms;       // [npad / 32][2][32] reference m of the rows' exponentials; weight scale / S, 0: no part in the gradient
     float2* rq;       // [npad] largest scaled teacher logit; S / Q, the share of the teacher in units of the exponentials
-    uint4* g0;        // [npad / 16][NG][64 lanes] operands of G: 0 for rows without a part in the gradient, NaN for rows that are NaN
-    uint4* gs;        // [npad / 32][KC][3][64 lanes] operands of rs G, finite
+    u32x4* g0;        // [npad / 16][NG][64 lanes] operands of G: 0 for rows without a part in the gradient, NaN for rows that are NaN
+    u32x4* gs;        // [npad / 32][KC][3][64 lanes] operands of rs G, finite
     // the teacher's entries of 32 rows by blocks of 2^entry_shift candidates: place in the block * 32 + row of the tile, share
     uint2* entries;   // [npad / 32][32 T]
     uint32_t* starts; // [npad / 32][entry_blocks + 1]

@@ -9,11 +9,10 @@
 
 namespace {
 
-// Order of logits as whole numbers: 0 for -infinity and NaN, which are never among the best.
+// Order of logits as whole numbers above 0.
 __device__ __forceinline__ uint32_t logit_key(float z)
 {
     z += 0.f;  // one zero
-    if (!(z > -INFINITY)) return 0;
     const uint32_t b = __float_as_uint(z);
     return (int32_t)b < 0 ? ~b : b | 0x80000000u;
 }
@@ -41,10 +40,10 @@ __device__ __forceinline__ FieldPart row_stats(const FieldArgs& A, int64_t row, 
 }
 
 // Order of an item of value z and number id: by value, lower numbers first among equal ones.  0: never among the best.
-__device__ __forceinline__ uint64_t item_key(float z, int64_t id)
+__device__ __forceinline__ uint64_t item_key(float z, float out, uint32_t id)
 {
-    const uint32_t k = logit_key(z);
-    return k == 0 ? 0 : (uint64_t)k << 32 | (uint32_t)~(uint32_t)id;
+    const uint32_t k = z > 0.5f * out ? logit_key(z) : 0;
+    return k == 0 ? 0 : (uint64_t)k << 32 | (uint32_t)~id;
 }
 __device__ __forceinline__ int64_t key_id(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 
@@ -60,15 +59,17 @@ struct SelectLds {
 };
 
 template <int BS, typename F, typename N>
-__device__ __forceinline__ void select_best(int64_t count, int top, uint64_t* best, SelectLds<BS>& lds, F value, N number)
+__device__ __forceinline__ void select_best(uint32_t count, int top, float out, uint64_t* best, SelectLds<BS>& lds, F value, N number)
 {
     const int tid = threadIdx.x;
-    uint64_t mine = 0;
+    float most = -INFINITY;
+    uint32_t where = 0;
 #pragma unroll 4
-    for (int64_t i = tid; i < count; i += BS) {
-        const uint64_t k = item_key(value(i), number(i));
-        mine = k > mine ? k : mine;
+    for (uint32_t i = tid; i < count; i += BS) {
+        const float v = value(i);
+        if (v > most) most = v, where = i;
     }
+    uint64_t mine = tid < count ? item_key(most, out, number(where)) : 0;
     lds.max[tid] = mine;
     if (tid == 0) lds.count = 0, lds.from = 1;
     for (int a = tid; a < top; a += BS) best[a] = 0;
@@ -87,9 +88,12 @@ __device__ __forceinline__ void select_best(int64_t count, int top, uint64_t* be
     for (;;) {
         __syncthreads();
         const uint64_t from = lds.from;
+        const float least = from == 1 ? -INFINITY : key_logit((uint32_t)(from >> 32));
 #pragma unroll 4
-        for (int64_t i = tid; i < count; i += BS) {
-            const uint64_t k = item_key(value(i), number(i));
+        for (uint32_t i = tid; i < count; i += BS) {
+            const float v = value(i);
+            if (v < least) continue;
+            const uint64_t k = item_key(v, out, number(i));
             if (k >= from) {
                 const int at = atomicAdd(&lds.count, 1);
                 if (at < SELECT_LIST) lds.list[at] = k;
@@ -171,24 +175,24 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
         }
     // of the parts of the candidates those with the largest maxima, of these the groups, of these the candidates
     const float* gm = A.gmax + row * A.blocks * 4;
-    const int64_t in_split = A.chunk / FM_BLOCK_CANDS * 4;  // groups
-    const bool all = A.splits <= 2 * A.top || A.splits * in_split <= 4 * BS;
+    const uint32_t in_split = (uint32_t)(A.chunk / FM_BLOCK_CANDS * 4), all_groups = (uint32_t)(A.blocks * 4);
+    const bool all = A.splits <= 2 * A.top || all_groups <= 64 * BS;
     int nsplits = A.splits, ng = 0;
-    const auto group = [&](int64_t i) {  // i-th group of the parts that were taken
-        return all ? i : groups[(int)(i / in_split)] * in_split + i % in_split;
+    const auto group = [&](uint32_t i) {  // i-th group of the parts that were taken
+        return all ? i : (uint32_t)groups[i / in_split] * in_split + i % in_split;
     };
-    const auto candidate = [&](int64_t i) {  // i-th candidate of the groups that were taken
-        const int64_t id = groups[i / 16];
+    const auto candidate = [&](uint32_t i) {  // i-th candidate of the groups that were taken
+        const uint32_t id = (uint32_t)groups[i / 16];
         return id / 4 * FM_BLOCK_CANDS + 4 * (id % 4) + i % 16 / 4 * 16 + i % 4;
     };
     for (int stage = all ? 1 : 0; stage < 3; ++stage) {
-        const int64_t count = nan ? 0 : stage == 0 ? A.splits : stage == 1 ? nsplits * in_split : 16 * ng;
-        select_best<BS>(count, A.top, best, lds, [&](int64_t i) {
-            if (stage == 0) return A.part[i * A.n + row].w;
+        const uint32_t count = nan ? 0 : stage == 0 ? A.splits : stage == 2 ? 16 * ng : all ? all_groups : nsplits * in_split;
+        select_best<BS>(count, A.top, A.out, best, lds, [&](uint32_t i) {
+            if (stage == 0) return A.part[(int64_t)i * A.n + row].w;
             if (stage == 2) return zs[i];
-            const int64_t at = group(i);
-            return at < A.blocks * 4 ? gm[at] : -INFINITY;
-        }, [&](int64_t i) { return stage == 0 ? i : stage == 1 ? group(i) : candidate(i); });
+            const uint32_t at = group(i);
+            return at < all_groups ? gm[at] : -INFINITY;
+        }, [&](uint32_t i) { return stage == 0 ? i : stage == 1 ? group(i) : candidate(i); });
         if (stage == 0) {
             nsplits = 0;
             for (int a = 0; a < A.top; ++a) nsplits += best[a] != 0;
@@ -200,7 +204,7 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
                 const int64_t id = key_id(k), other = id / 4 * 4 + i % 4;
                 bool take = other == id;
                 if (!take) {  // equal to the last one that was taken, and not taken itself
-                    const uint64_t last = best[A.top - 1], mine = item_key(gm[other], other);
+                    const uint64_t last = best[A.top - 1], mine = item_key(gm[other], A.out, (uint32_t)other);
                     take = last != 0 && mine < last && mine >> 32 == last >> 32;
                     for (int o = 0; take && o < i / 4; ++o) take = best[o] == 0 || key_id(best[o]) / 4 != id / 4;  // once for the block
                 }
@@ -235,6 +239,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
     float* factor = reinterpret_cast<float*>(entries + A.T);
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
+    float* rms = A.rms + row / 32 * 64 + row % 32;
     // the row's part of the operands: k0..k0 + 3 of G as the logits take it, and of rs G
     const auto lay_out = [&](int k0, f32x4 x, f32x4 y) {
         using Ops = FieldOps<FmParts<TV>::value, KC>;
@@ -260,7 +265,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
     };
     if (row >= A.n) {
         for (int k = 4 * tid; k < KP; k += 4 * BS) lay_out(k, f32x4{}, f32x4{});
-        if (tid == 0) A.rm[row] = 3e38f, A.rs[row] = 0.f, A.rq[row] = make_float2(0.f, 0.f);
+        if (tid == 0) rms[0] = 3e38f, rms[32] = 0.f, A.rq[row] = make_float2(0.f, 0.f);
         return;
     }
     for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
@@ -318,8 +323,8 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
     const float rs = counts ? r / p.S : 0.f;
     if (tid == 0) {
         if (A.loss != nullptr) A.loss[row] = x;
-        A.rm[row] = !counts ? 3e38f : nan ? 0.f : p.m;
-        A.rs[row] = nan ? 0.f : rs;
+        rms[0] = !counts ? 3e38f : nan ? 0.f : p.m;
+        rms[32] = nan ? 0.f : rs;
         A.rq[row] = make_float2(mt, counts && !nan ? p.S / Q : 0.f);
     }
     for (int k = 4 * tid; k < KP; k += 4 * BS) {
@@ -363,7 +368,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
     }
 }
 
-// Lists of the teacher's entries of 32 rows by blocks of candidates.  Order inside a block does not matter: every entry has a
+// Lists of the teacher's entries of 32 rows, those that the row allows, by blocks of candidates.  Order inside a block does not matter: every entry has a
 // place of its own in the tile of the candidates' kernel.
 __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
 {
@@ -379,7 +384,8 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
             const int64_t j = A.ids[(int64_t)i0 * A.T + i];
             if (j < 0 || j >= A.C) continue;
             const float2 q = A.rq[i0 + r];
-            if (q.y != 0.f) take(r, j, q, i);
+            if (q.y == 0.f || !fm_field_allowed(A, i0 + r, j) || (A.w != nullptr && A.w[j] == -INFINITY)) continue;
+            take(r, j, q, i);
         }
     };
     each([&](uint32_t, int64_t j, float2, uint32_t) { atomicAdd(&place[j >> A.entry_shift], 1u); });
@@ -411,7 +417,11 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
     });
 }
 
-constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most and if there is as much to do
+#ifndef ROWITEMS
+#define ROWITEMS 8192
+#define COLITEMS 8192
+#endif
+constexpr int FIELD_ROW_ITEMS = ROWITEMS, FIELD_COL_ITEMS = COLITEMS;                        // wavefronts that a sweep is split into, at most and if there is as much to do
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
 constexpr int64_t FIELD_WIDE_ROWS = 2048;                // below, a row gets a workgroup of four wavefronts, else one
@@ -462,7 +472,7 @@ int32_t entry_shift(int64_t C, int64_t rows)
 
 // Where the pieces of the workspace begin.  The maxima of groups (logprobs) and what distillation needs share their place.
 struct Layout {
-    size_t part, gmax, opart, rm, rs, rq, g0, gs, entries, starts, wpart, vpart, pv, pt, pw, bytes;
+    size_t part, gmax, opart, rms, rq, g0, gs, entries, starts, wpart, vpart, pv, pt, pw, bytes;
     explicit Layout(const fm_field* f)
     {
         size_t at = 0;
@@ -480,8 +490,7 @@ struct Layout {
         gmax = opart = at;
         const size_t top = at + room(f->top_rows * up(f->C, FM_BLOCK_CANDS) * 16);
         take(distill ? f->slots * KP * 4 : 0);
-        rm = take(rows * 4);
-        rs = take(rows * 4);
+        rms = take(rows * 8);
         rq = take(rows * 8);
         g0 = take(rows / 16 * 1024 * (KC == 1 ? 3 : 3 * KC / 2));
         gs = take(rows / 32 * 1024 * 3 * KC);
@@ -534,12 +543,13 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.n = (int32_t)n;
     A.scale = c->scale;
     A.sl = c->scale * FM_LOG2E;
+    A.out = -std::min(1e30f, 1e36f / A.sl);
     A.packed = f->packs && n > FIELD_DIRECT_ROWS;
     const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed);
     A.row_tiles = (int32_t)up(n, per);
     // straight from V a part of the candidates is shared by the wavefronts of a workgroup
     const int64_t share = A.packed ? 1 : FM_FIELD_SHARE, blocks = up(f->C, FM_BLOCK_CANDS);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / share / std::max(A.row_tiles, 1), up(blocks, share)));
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(FIELD_ROW_ITEMS / share / std::max(A.row_tiles, 1), up(blocks, share)));
     A.chunk = up(blocks, splits) * FM_BLOCK_CANDS;
     A.splits = (int32_t)up(f->C, A.chunk);
     A.blocks = up(f->C, FM_BLOCK_CANDS);
@@ -548,13 +558,12 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.part = reinterpret_cast<float4*>(f->block + at.part);
     A.gmax = floats(at.gmax);
     A.opart = floats(at.opart);
-    A.rm = floats(at.rm);
-    A.rs = floats(at.rs);
+    A.rms = floats(at.rms);
     A.rq = reinterpret_cast<float2*>(f->block + at.rq);
-    A.g0 = reinterpret_cast<uint4*>(f->block + at.g0);
-    A.gs = reinterpret_cast<uint4*>(f->block + at.gs);
-    A.pv = reinterpret_cast<uint4*>(f->block + at.pv);
-    A.pt = reinterpret_cast<uint4*>(f->block + at.pt);
+    A.g0 = reinterpret_cast<u32x4*>(f->block + at.g0);
+    A.gs = reinterpret_cast<u32x4*>(f->block + at.gs);
+    A.pv = reinterpret_cast<u32x4*>(f->block + at.pv);
+    A.pt = reinterpret_cast<u32x4*>(f->block + at.pt);
     A.pw = floats(at.pw);
     A.entries = reinterpret_cast<uint2*>(f->block + at.entries);
     A.starts = reinterpret_cast<uint32_t*>(f->block + at.starts);
@@ -564,7 +573,7 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.entry_shift = entry_shift(f->C, f->max_rows);
     A.entry_blocks = (int32_t)up(f->C, int64_t(1) << A.entry_shift);
     A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 32));
+    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_COL_ITEMS / A.col_tiles, A.npad / 32));
     A.row_chunk = (int32_t)std::max<int64_t>(32, up(up(A.npad, parts), 32) * 32);
     A.row_splits = (int32_t)std::max<int64_t>(1, up(A.npad, A.row_chunk));
     return A;
@@ -609,10 +618,10 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     f->max_top = max_top;
     f->max_entries = max_entries;
     f->packs = max_rows > FIELD_DIRECT_ROWS && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
-    // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
-    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
+    // of n rows in tiles of `per`: at most FIELD_ROW_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
+    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ROW_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
     const int64_t tiles = up(C, fm_field_cols_per_wave(K));
-    const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole32(max_rows) / 32);
+    const int64_t col_parts = std::min(FIELD_COL_ITEMS / tiles, whole32(max_rows) / 32);
     f->col_parts = col_parts > 1 && max_entries > 0 ? C * col_parts : 0;  // a single part is written to where it belongs
     f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / (4 * up(C, FM_BLOCK_CANDS))));
     const size_t bytes = Layout(f).bytes;

@@ -14,23 +14,42 @@ __device__ __forceinline__ void wave_sync()
 // A wavefront takes 16 NT candidates and a part of the rows, 32 of them at a time.  The tiles of logits have rows down and
 // candidates across, so that they are the B operand of the second product (rows are what it sums over) as they stand:
 //   grad_V^T[k][j] += gs[i][k] P[i][j],   P_ij = 2^(x_ij - m_i) - (share of the teacher),   gs = weight scale / S G.
-// The teacher's few entries come into the tiles by way of LDS.
+// The teacher's few entries, none of them left out, come into the tiles by way of LDS.
+template <int KC>
+struct ColsShape {
+    static constexpr int NG = FieldOps<3, KC>::NG, NG1 = FieldOps<1, KC>::NG;  // KC = 1: 2 operands of G against bfloat16 values
+    template <int NP> static constexpr int ops() { return 2 * FieldOps<NP, KC>::NG + 3 * KC; }
+    static constexpr int W = fm_field_waves(2 * NG + 3 * KC);
+    static constexpr bool STAGED = fm_field_staged(2 * NG + 3 * KC);
+};
+
 template <typename TV, int KC, int FILL, int NT>
-__global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
+__global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_field_cols(const FieldArgs A)
 {
     constexpr int NP = FmParts<TV>::value, KP = 16 * KC, QS = 36;  // QS: floats to a candidate of the tile in LDS, 32 rows
     using Ops = FieldOps<NP, KC>;
-    __shared__ __align__(16) float teacher[FM_WAVES][16 * NT * QS];
-    const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
-    const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (item >= (int64_t)A.col_tiles * A.row_splits) return;
-    const int64_t c0 = item % A.col_tiles * (16 * NT);
-    const int split_no = (int)(item / A.col_tiles);
+    constexpr int W = ColsShape<KC>::W, OPS = ColsShape<KC>::template ops<NP>(), EXTRA = 16;
+    constexpr bool STAGED = ColsShape<KC>::STAGED;
+    __shared__ __align__(16) float teacher[W][16 * NT * QS];
+    extern __shared__ u32x4 stages[];  // [2][OPS * 64 + EXTRA]
+    const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    // parts of the rows one after the other: candidates that many rows name, and that take longer for it, are often the first ones
+    const int64_t tile = (int64_t)(blockIdx.x / A.row_splits) * W + wave;
+    const int split_no = (int)(blockIdx.x % A.row_splits);
+    const bool idle = tile >= A.col_tiles;  // goes along for the barriers
+    const int64_t c0 = idle ? 0 : tile * (16 * NT);
     const int beg = split_no * A.row_chunk, end = min(A.npad, beg + A.row_chunk);
     const TV* V = static_cast<const TV*>(A.V);
-    float* Q = teacher[threadIdx.x / 64];
+    float* Q = teacher[wave];
     for (int i = lane; i < 16 * NT * QS; i += 64) Q[i] = 0.f;
     wave_sync();
+
+    FieldStage<OPS, EXTRA, 64 * W> next;
+    const auto ask = [&](int i0) {
+        next.ask(A.g0 + (int64_t)(i0 / 16) * Ops::NG * 64, 2 * Ops::NG * 64, A.gs + (int64_t)(i0 / 32) * KC * 3 * 64, KC * 3 * 64,
+                 reinterpret_cast<const u32x4*>(A.rms) + i0 / 32 * 16);
+    };
+    if (STAGED && beg < end) ask(beg);
 
     bf16x8 b[NT][Ops::NV];
     f32x4 w[NT], acc[KC][NT];
@@ -54,63 +73,84 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
         Ops::of_v(p, b[t]);
     }
     const bool row_masks = A.mask != nullptr && A.mask_stride != 0;
+    const uint32_t* mask = row_masks ? A.mask + (c0 >> 5) : nullptr;
+    const int64_t last_word = row_masks ? ((A.C - 1) >> 5) - (c0 >> 5) : 0;
     const uint32_t* starts = A.starts + (c0 >> A.entry_shift);
     const uint32_t in_block = (uint32_t)(c0 & ((int64_t(1) << A.entry_shift) - 1));
+    // the entries of a tile of rows, the same range in all lanes, and the first 64 of them: asked for a tile ahead
+    uint32_t from_next = 0, to_next = 0;
+    uint2 entry_next = make_uint2(0, 0);
+    const auto named = [&](int i0) {
+        const uint32_t* range = starts + (int64_t)(i0 / 32) * (A.entry_blocks + 1);
+        from_next = __builtin_amdgcn_readfirstlane(range[0]);
+        to_next = idle ? from_next : __builtin_amdgcn_readfirstlane(range[1]);
+        if (from_next + lane < to_next) entry_next = A.entries[(int64_t)i0 * A.T + from_next + lane];
+    };
+    if (beg < end) named(beg);
+    if (STAGED && beg < end) {
+        next.put(stages);
+        __syncthreads();
+    }
 
     for (int i0 = beg; i0 < end; i0 += 32) {
-        f32x4 z[2][NT], m[2], rs[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            bf16x8 a[Ops::NG];
-#pragma unroll
-            for (int o = 0; o < Ops::NG; ++o) a[o] = __builtin_bit_cast(bf16x8, A.g0[((int64_t)(i0 / 16 + h) * Ops::NG + o) * 64 + lane]);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) z[h][t] = Ops::template product<false>(b[t], a, w[t]);
-            m[h] = *reinterpret_cast<const f32x4*>(A.rm + i0 + 16 * h + 4 * g);
-            rs[h] = *reinterpret_cast<const f32x4*>(A.rs + i0 + 16 * h + 4 * g);
-        }
-        if (row_masks) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const uint32_t* words = A.mask + min(i0 + 16 * h + 4 * g + r, A.n - 1) * A.mask_stride;
-#pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        const int64_t j = min(c0 + 16 * t + lo, A.C - 1);
-                        z[h][t][r] = words[j >> 5] >> (j & 31) & 1u ? z[h][t][r] : -INFINITY;
-                    }
-                }
-        }
-        const auto exponential = [&](int h, int t, int r) { return __builtin_amdgcn_exp2f(fmaf(z[h][t][r], A.sl, -m[h][r])); };
-        const uint32_t* range = starts + (int64_t)(i0 / 32) * (A.entry_blocks + 1);
-        const uint32_t from = range[0], to = range[1];  // the same in all lanes
+        const u32x4* ops = STAGED ? stages + (i0 - beg) / 32 % 2 * (OPS * 64 + EXTRA) : A.g0 + (int64_t)(i0 / 16) * Ops::NG * 64;
+        const u32x4* gs = STAGED ? ops + 2 * Ops::NG * 64 : A.gs + (int64_t)(i0 / 32) * KC * 3 * 64;
+        const f32x4* ms = STAGED ? reinterpret_cast<const f32x4*>(ops + OPS * 64) : reinterpret_cast<const f32x4*>(A.rms) + i0 / 32 * 16;
+        if (STAGED && i0 + 32 < end) ask(i0 + 32);
+        const uint2* entries = A.entries + (int64_t)i0 * A.T;
+        const uint32_t from = from_next, to = to_next;
+        const uint2 entry = entry_next;
+        named(i0 + 32 < end ? i0 + 32 : i0);
         if (from != to) {
-            const uint2* entries = A.entries + (int64_t)i0 * A.T;
             for (uint32_t i = from + lane; i < to; i += 64) {
-                const uint2 e = entries[i];
+                const uint2 e = i < from + 64 ? entry : entries[i];
                 const uint32_t j = (e.x >> 5) - in_block;
                 if (j < 16 * NT) atomicAdd(&Q[j * QS + (e.x & 31)], __uint_as_float(e.y));  // into zero but for ids that come twice
             }
             wave_sync();
+        }
+        uint32_t words[2][4][(NT + 1) / 2];
+        if (row_masks)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int i = 0; i < (NT + 1) / 2; ++i)
+                        words[h][r][i] = mask[min(i0 + 16 * h + 4 * g + r, A.n - 1) * A.mask_stride + min((int64_t)i, last_word)];
+        f32x4 z[2][NT], rs[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            bf16x8 a[Ops::NG];
+#pragma unroll
+            for (int o = 0; o < Ops::NG; ++o) a[o] = __builtin_bit_cast(bf16x8, ops[(h * Ops::NG + o) * 64 + lane]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) z[h][t] = Ops::template product<false>(b[t], a, w[t]);
+            if (row_masks)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int bit = (NT == 1 ? (int)(c0 & 31) : 16 * (t % 2)) + lo;
+                        z[h][t][r] = words[h][r][t / 2] >> bit & 1u ? z[h][t][r] : -INFINITY;
+                    }
+            const f32x4 m = ms[4 * h + g];
+            rs[h] = ms[8 + 4 * h + g];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) z[h][t][r] = __builtin_amdgcn_exp2f(fmaf(z[h][t][r], A.sl, -m[r]));
+        }
+        if (from != to) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     f32x4* at = reinterpret_cast<f32x4*>(Q + (16 * t + lo) * QS + 16 * h + 4 * g);
-                    const f32x4 q = *at;
+                    z[h][t] -= *at;
                     *at = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[h][t][r] = exponential(h, t, r) - (z[h][t][r] == -INFINITY ? 0.f : q[r]);
                 }
             wave_sync();
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) z[h][t][r] = exponential(h, t, r);
         }
         bf16x8 e[NT][3];
 #pragma unroll
@@ -129,13 +169,19 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_cols(const FieldArgs A)
         for (int c = 0; c < KC; ++c)
 #pragma unroll
             for (int p = 2; p >= 0; --p) {
-                const bf16x8 a = __builtin_bit_cast(bf16x8, A.gs[((int64_t)(i0 / 32 * KC + c) * 3 + p) * 64 + lane]);
+                const bf16x8 a = __builtin_bit_cast(bf16x8, gs[(c * 3 + p) * 64 + lane]);
 #pragma unroll
                 for (int q = 2 - p; q >= 0; --q)
 #pragma unroll
                     for (int t = 0; t < NT; ++t) acc[c][t] = mfma32(a, e[t][q], acc[c][t]);
             }
+        if (STAGED && i0 + 32 < end) {
+            // the other stage was read before the last barrier
+            next.put(stages + ((i0 - beg) / 32 + 1) % 2 * (OPS * 64 + EXTRA));
+            __syncthreads();
+        }
     }
+    if (idle) return;
 
     const bool whole = A.row_splits == 1;
 #pragma unroll
@@ -188,11 +234,13 @@ int fm_field_cols_per_wave(int32_t K) { return 16 * fm_field_col_tiles(fm_field_
 
 void fm_field_cols(int32_t v_type, const FieldArgs& A, hipStream_t st)
 {
-    const int64_t items = (int64_t)A.col_tiles * A.row_splits;
     fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto fill) {
-        constexpr int KC = decltype(kc)::value;
-        k_field_cols<decltype(type), KC, decltype(fill)::value, fm_field_col_tiles(KC)>
-            <<<(uint32_t)((items + FM_WAVES - 1) / FM_WAVES), FM_BLOCK, 0, st>>>(A);
+        using TV = decltype(type);
+        constexpr int KC = decltype(kc)::value, W = ColsShape<KC>::W;
+        constexpr size_t lds = ColsShape<KC>::STAGED ? 2 * (ColsShape<KC>::template ops<FmParts<TV>::value>() * 64 + 16) * sizeof(u32x4) : 0;
+        const auto kernel = k_field_cols<TV, KC, decltype(fill)::value, fm_field_col_tiles(KC)>;
+        if (lds > 48 * 1024) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        kernel<<<(uint32_t)((A.col_tiles + W - 1) / W * A.row_splits), 64 * W, lds, st>>>(A);
     });
     if (A.row_splits == 1) return;
     const int KP = 16 * fm_field_chunks(A.K);

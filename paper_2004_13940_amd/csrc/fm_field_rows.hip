@@ -12,13 +12,13 @@ struct RowStats {
     float m[NT], S[NT], U[NT], best[NT];
     f32x4 o[DISTILL ? KC : 1][NT];
 
-    __device__ __forceinline__ RowStats()
+    __device__ __forceinline__ explicit RowStats(const FieldArgs& A)
     {
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            m[t] = -3e38f;
+            m[t] = 0.5f * A.out * A.sl;  // above all that is left out
             S[t] = U[t] = 0.f;
-            best[t] = -INFINITY;
+            best[t] = A.out;
 #pragma unroll
             for (int c = 0; c < (DISTILL ? KC : 1); ++c) o[c][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
@@ -69,7 +69,7 @@ struct RowStats {
             if constexpr (DISTILL)
                 z[r] = e;
             else
-                U[t] = fmaf(e, fmaxf(x, -200.f), U[t]);  // e is 0 where x is -infinity
+                U[t] = fmaf(e, x, U[t]);
         }
     }
 
@@ -104,15 +104,15 @@ struct RowStats {
     }
 };
 
-// -infinity for what the mask words of a row leave out of a block: bits[h] are candidates 32 h..32 h + 31 of it.
+// What the mask words of a row leave out of a block: bits[h] are candidates 32 h..32 h + 31 of it.
 template <int NT>
-__device__ __forceinline__ void leave_out(f32x4 (&z)[4][NT], int t, const uint32_t (&bits)[2], int g)
+__device__ __forceinline__ void leave_out(f32x4 (&z)[4][NT], int t, const uint32_t (&bits)[2], int g, float out)
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t four = bits[i / 2] >> (16 * (i % 2) + 4 * g);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) z[i][t][r] = four >> r & 1u ? z[i][t][r] : -INFINITY;
+        for (int r = 0; r < 4; ++r) z[i][t][r] = four >> r & 1u ? z[i][t][r] : out;
     }
 }
 
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
             finite_or_nan(b[t][c]);
         }
     }
-    RowStats<KC, NT, DISTILL> s;
+    RowStats<KC, NT, DISTILL> s(A);
     for (int64_t j0 = beg + wave * FM_BLOCK_CANDS; j0 < end; j0 += W * FM_BLOCK_CANDS) {
         f32x4 z[4][NT];
 #pragma unroll
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
             f32x4 w = {0.f, 0.f, 0.f, 0.f};
             if (A.w != nullptr)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) w[r] = A.w[min(j0 + 16 * i + 4 * g + r, A.C - 1)];
+                for (int r = 0; r < 4; ++r) w[r] = fmaxf_or_nan(A.w[min(j0 + 16 * i + 4 * g + r, A.C - 1)], A.out);
 #pragma unroll
             for (int t = 0; t < NT; ++t) z[i][t] = w;
 #pragma unroll
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
                     bits[h] = left <= 0 ? 0u : left < 32 ? (1u << left) - 1u : ~0u;
                     if (A.mask != nullptr && left > 0) bits[h] &= A.mask[mask_row[t] + (j0 >> 5) + h];
                 }
-                leave_out(z, t, bits, g);
+                leave_out(z, t, bits, g, A.out);
             }
         }
         float top[NT];
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_pack(const FieldArgs A)
     const auto there = [&](int64_t j) { return j < A.C && (!shared || (A.mask[j >> 5] >> (j & 31) & 1u) != 0); };
     if (lane < 32) {
         const int64_t j = tile * 32 + lane;
-        A.pw[j] = !there(j) ? -INFINITY : A.w != nullptr ? A.w[j] : 0.f;
+        A.pw[j] = !there(j) ? A.out : A.w != nullptr ? fmaxf_or_nan(A.w[j], A.out) : 0.f;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -277,7 +277,7 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_pack(const FieldArgs A)
         }
         Ops::of_v(p, ops);
 #pragma unroll
-        for (int o = 0; o < Ops::NV; ++o) A.pv[((tile * 2 + h) * Ops::NV + o) * 64 + lane] = __builtin_bit_cast(uint4, ops[o]);
+        for (int o = 0; o < Ops::NV; ++o) A.pv[((tile * 2 + h) * Ops::NV + o) * 64 + lane] = __builtin_bit_cast(u32x4, ops[o]);
     }
     if constexpr (DISTILL) {
 #pragma unroll
@@ -297,23 +297,39 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_pack(const FieldArgs A)
             }
 #pragma unroll
             for (int q = 0; q < NP; ++q)
-                A.pt[((tile * KC + c) * NP + q) * 64 + lane] = __builtin_bit_cast(uint4, join(p[0][q], p[1][q]));
+                A.pt[((tile * KC + c) * NP + q) * 64 + lane] = __builtin_bit_cast(u32x4, join(p[0][q], p[1][q]));
         }
     }
 }
 
 // The same as k_field_rows from the packed table, products as sums of bfloat16 ones.
+template <int NP, int KC, bool DISTILL>
+struct RowsShape {
+    static constexpr int NV = FieldOps<NP, KC>::NV, OPS = 4 * NV + (DISTILL ? 2 * KC * NP : 0);  // to a block of 64 candidates
+    static constexpr int W = fm_field_waves(OPS);
+    static constexpr bool STAGED = fm_field_staged(OPS);
+};
+
 template <int NP, int KC, int NT, bool DISTILL>
-__global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldArgs A)
+__global__ __launch_bounds__((64 * RowsShape<NP, KC, DISTILL>::W), KC == 16 ? 1 : 2) void k_field_rows_packed(const FieldArgs A)
 {
     using Ops = FieldOps<NP, KC>;
-    const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16;
-    const int64_t item = (int64_t)blockIdx.x * FM_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (item >= (int64_t)A.row_tiles * A.splits) return;
-    const int split_no = (int)(item / A.row_tiles), row0 = (int)(item % A.row_tiles) * 16 * NT;
+    using Shape = RowsShape<NP, KC, DISTILL>;
+    constexpr int W = Shape::W, OPS = Shape::OPS, EXTRA = 16;
+    constexpr bool STAGED = Shape::STAGED;
+    extern __shared__ u32x4 stages[];  // [2][OPS * 64 + EXTRA]
+    const int lane = threadIdx.x % 64, lo = lane % 16, g = lane / 16, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int groups = (A.row_tiles + W - 1) / W;
+    const int split_no = (int)blockIdx.x / groups, row0 = ((int)blockIdx.x % groups * W + wave) * 16 * NT;
     const int64_t beg = split_no * A.chunk, end = min(A.C, beg + A.chunk);
     const bool row_masks = A.mask != nullptr && A.mask_stride != 0;
 
+    FieldStage<OPS, EXTRA, 64 * W> next;
+    const auto ask = [&](int64_t j0) {
+        next.ask(A.pv + j0 / 16 * Ops::NV * 64, 4 * Ops::NV * 64, A.pt + j0 / 32 * KC * NP * 64, DISTILL ? 2 * KC * NP * 64 : 0,
+                 reinterpret_cast<const u32x4*>(A.pw) + j0 / 4);
+    };
+    if (STAGED) ask(beg);
     bf16x8 b[NT][Ops::NG];
     int64_t mask_row[NT];
 #pragma unroll
@@ -330,15 +346,23 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldAr
         }
         Ops::of_g(p, b[t]);
     }
-    RowStats<KC, NT, DISTILL> s;
+    if (STAGED) {
+        next.put(stages);
+        __syncthreads();
+    }
+    RowStats<KC, NT, DISTILL> s(A);
     for (int64_t j0 = beg; j0 < end; j0 += FM_BLOCK_CANDS) {
+        const u32x4* pv = STAGED ? stages + (uint32_t)(j0 - beg) / FM_BLOCK_CANDS % 2 * (OPS * 64 + EXTRA) : A.pv + j0 / 16 * Ops::NV * 64;
+        const u32x4* pt = STAGED ? pv + 4 * Ops::NV * 64 : A.pt + j0 / 32 * KC * NP * 64;
+        const f32x4* pw = STAGED ? reinterpret_cast<const f32x4*>(pv + OPS * 64) : reinterpret_cast<const f32x4*>(A.pw + j0);
+        if (STAGED && j0 + FM_BLOCK_CANDS < end) ask(j0 + FM_BLOCK_CANDS);
         f32x4 z[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             bf16x8 a[Ops::NV];
 #pragma unroll
-            for (int o = 0; o < Ops::NV; ++o) a[o] = __builtin_bit_cast(bf16x8, A.pv[((j0 / 16 + i) * Ops::NV + o) * 64 + lane]);
-            const f32x4 w = *reinterpret_cast<const f32x4*>(A.pw + j0 + 16 * i + 4 * g);
+            for (int o = 0; o < Ops::NV; ++o) a[o] = __builtin_bit_cast(bf16x8, pv[(i * Ops::NV + o) * 64 + lane]);
+            const f32x4 w = pw[4 * i + g];
 #pragma unroll
             for (int t = 0; t < NT; ++t) z[i][t] = Ops::template product<true>(a, b[t], w);
         }
@@ -347,8 +371,8 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldAr
             for (int t = 0; t < NT; ++t) {
                 uint32_t bits[2];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) bits[h] = j0 + 32 * h < A.C ? A.mask[mask_row[t] + (j0 >> 5) + h] : 0u;
-                leave_out(z, t, bits, g);
+                for (int h = 0; h < 2; ++h) bits[h] = A.mask[mask_row[t] + min((j0 >> 5) + h, (A.C - 1) >> 5)];
+                leave_out(z, t, bits, g, A.out);
             }
         }
         float top[NT];
@@ -374,13 +398,18 @@ __global__ __launch_bounds__(FM_BLOCK, 2) void k_field_rows_packed(const FieldAr
                 for (int c = 0; c < KC; ++c)
 #pragma unroll
                     for (int p = NP - 1; p >= 0; --p) {
-                        const bf16x8 a = __builtin_bit_cast(bf16x8, A.pt[(((j0 + 16 * i) / 32 * KC + c) * NP + p) * 64 + lane]);
+                        const bf16x8 a = __builtin_bit_cast(bf16x8, pt[((i / 2 * KC + c) * NP + p) * 64 + lane]);
 #pragma unroll
                         for (int q = 2 - p; q >= 0; --q)
 #pragma unroll
                             for (int t = 0; t < NT; ++t) s.o[c][t] = mfma32(a, e[t][q], s.o[c][t]);
                     }
             }
+        }
+        if (STAGED && j0 + FM_BLOCK_CANDS < end) {
+            // the other stage was read before the last barrier
+            next.put(stages + ((uint32_t)(j0 - beg) / FM_BLOCK_CANDS + 1) % 2 * (OPS * 64 + EXTRA));
+            __syncthreads();
         }
     }
     s.join();
@@ -395,10 +424,13 @@ void rows(int32_t v_type, const FieldArgs& A, hipStream_t st)
     fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto fill) {
         using TV = decltype(type);
         constexpr int KC = decltype(kc)::value, FILL = decltype(fill)::value;
-        const uint32_t grid = blocks_of((int64_t)A.row_tiles * A.splits);
         if (A.packed) {
             k_field_pack<TV, KC, FILL, DISTILL><<<blocks_of(A.blocks * 2), FM_BLOCK, 0, st>>>(A);
-            k_field_rows_packed<FmParts<TV>::value, KC, fm_field_row_tiles(KC, DISTILL), DISTILL><<<grid, FM_BLOCK, 0, st>>>(A);
+            using Shape = RowsShape<FmParts<TV>::value, KC, DISTILL>;
+            constexpr size_t lds = Shape::STAGED ? 2 * (Shape::OPS * 64 + 16) * sizeof(u32x4) : 0;
+            const auto kernel = k_field_rows_packed<FmParts<TV>::value, KC, fm_field_row_tiles(KC, DISTILL), DISTILL>;
+            if (lds > 48 * 1024) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+            kernel<<<(uint32_t)((A.row_tiles + Shape::W - 1) / Shape::W * A.splits), 64 * Shape::W, lds, st>>>(A);
         } else {
             k_field_rows<TV, KC, FILL, DISTILL><<<(uint32_t)(A.row_tiles * A.splits), 64 * FM_FIELD_SHARE, 0, st>>>(A);
         }

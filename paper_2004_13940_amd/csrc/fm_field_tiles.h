@@ -27,10 +27,20 @@ __device__ __forceinline__ f32x4 mfma32(bf16x8 a, bf16x8 b, f32x4 c) { return __
 template <int PARTS>
 __device__ __forceinline__ void split(f32x4 x, bf16x4 (&p)[PARTS])
 {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 #pragma unroll
     for (int i = 0; i < PARTS; ++i) {
-        p[i] = __builtin_convertvector(x, bf16x4);
-        if (i + 1 < PARTS) x -= __builtin_convertvector(p[i], f32x4);
+        uint32_t two[2];  // two roundings an instruction; what they stand for are their bits, above 16 zeros
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            two[h] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x[2 * h], x[2 * h + 1]}), bf16x2));
+            if (i + 1 < PARTS) {
+                x[2 * h] -= __uint_as_float(two[h] << 16);
+                x[2 * h + 1] -= __uint_as_float(two[h] & 0xFFFF0000u);
+            }
+        }
+        p[i] = __builtin_bit_cast(bf16x4, make_uint2(two[0], two[1]));
     }
 }
 __device__ __forceinline__ bf16x8 join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
@@ -104,6 +114,9 @@ struct FieldOps {
 // The nearest finite value: times a probability of 0 it is 0.
 __device__ __forceinline__ float finite(float v) { return __builtin_amdgcn_fmed3f(v, -FLT_MAX, FLT_MAX); }
 
+// The larger one; NaN if the first is.
+__device__ __forceinline__ float fmaxf_or_nan(float a, float b) { return a < b ? b : a; }
+
 // Infinite values count as NaN.
 __device__ __forceinline__ void finite_or_nan(float (&v)[4])
 {
@@ -132,8 +145,52 @@ __device__ __forceinline__ void load4(const T* row, int k, int K, float (&v)[4])
 // Chunks of 16 latent values that the kernels for K have: 1, 2, 4, 8 or 16.
 constexpr int fm_field_chunks(int32_t K) { return K <= 16 ? 1 : K <= 32 ? 2 : K <= 64 ? 4 : K <= 128 ? 8 : 16; }
 // Tiles of 16 rows, or of 16 candidates, that stay in a wavefront's registers: 256 of them are to do.
-constexpr int fm_field_row_tiles(int KC, bool distill) { return KC <= (distill ? 1 : 2) ? 4 : KC <= (distill ? 4 : 8) ? 2 : 1; }
-constexpr int fm_field_col_tiles(int KC) { return KC <= 1 ? 4 : KC <= 4 ? 2 : 1; }
+#ifndef LPNT1
+#define LPNT1 4
+#define LPNT4 2
+#define DSNT1 2
+#define DSNT4 2
+#define CNT1 4
+#define CNT4 2
+#endif
+constexpr int fm_field_row_tiles(int KC, bool distill) { return distill ? (KC == 1 ? DSNT1 : KC <= 4 ? DSNT4 : 1) : (KC <= 2 ? LPNT1 : KC <= 8 ? LPNT4 : 1); }
+constexpr int fm_field_col_tiles(int KC) { return KC <= 1 ? CNT1 : KC <= 4 ? CNT4 : 1; }
+
+// Operands that the wavefronts of a workgroup read in turn, 1 KB each, go through LDS in two stages: of so many operands to a
+// stage, four wavefronts to a workgroup, eight where two workgroups would not fit a compute unit, and straight from the
+// caches where one does not.
+constexpr int fm_field_waves(int ops) { return ops <= 32 ? 4 : 8; }
+#ifndef STAGEMAX
+#define STAGEMAX 64
+#endif
+constexpr bool fm_field_staged(int ops) { return ops <= STAGEMAX; }
+
+// A stage of OPS operands and EXTRA single values of 16 bytes on its way from memory to LDS: asked for while the one before it
+// is worked on, written when that is done.
+template <int OPS, int EXTRA, int THREADS>
+struct FieldStage {
+    static constexpr int COUNT = OPS * 64 + EXTRA, EACH = (COUNT + THREADS - 1) / THREADS;
+    u32x4 x[EACH];
+
+    // pieces: up to three stretches of memory, one after the other
+    __device__ __forceinline__ void ask(const u32x4* a, int na, const u32x4* b, int nb, const u32x4* c)
+    {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = i * THREADS + (int)threadIdx.x;
+            const u32x4* from = at < na ? a + at : at < na + nb ? b + (at - na) : c + (at - na - nb);
+            if ((i + 1) * THREADS <= COUNT || at < COUNT) x[i] = *from;
+        }
+    }
+    __device__ __forceinline__ void put(u32x4* lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = i * THREADS + (int)threadIdx.x;
+            if ((i + 1) * THREADS <= COUNT || at < COUNT) lds[at] = x[i];
+        }
+    }
+};
 
 constexpr int FM_FIELD_SHARE = 8;  // wavefronts to a part of the candidates in calls with few rows
 
@@ -169,5 +226,6 @@ void fm_field_shape(int32_t v_type, int32_t K, F run)
 int fm_field_rows_per_wave(bool distill, int32_t K, bool packed);
 void fm_field_rows(bool distill, int32_t v_type, const FieldArgs& A, hipStream_t st);  // through the packed table where A.packed
 int fm_field_cols_per_wave(int32_t K);
+
 int64_t fm_field_pack_bytes(bool distill, int32_t K, int64_t C);  // of the largest type
 void fm_field_cols(int32_t v_type, const FieldArgs& A, hipStream_t st);
