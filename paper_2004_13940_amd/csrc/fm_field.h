@@ -16,18 +16,27 @@ struct FieldPart {
     float m, S, U;
 };
 
+// The order of the two does not matter, to the last bit.
 __device__ __forceinline__ FieldPart fm_field_merge(FieldPart a, FieldPart b)
 {
     if (b.S == 0.f) return a;  // not so if S is NaN
     if (a.S == 0.f) return b;
+    const bool swap = b.m > a.m;
+    const FieldPart x = swap ? b : a, y = swap ? a : b;
+    const float d = y.m - x.m, f = __builtin_amdgcn_exp2f(d);
     FieldPart r;
-    r.m = fmaxf(a.m, b.m);
-    const float da = a.m - r.m, db = b.m - r.m;
-    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-    r.S = fa * a.S + fb * b.S;
-    // 0 times -infinity (a part 2^200 below the other) must not become NaN
-    r.U = (fa > 0.f ? fa * (a.U + da * a.S) : 0.f) + (fb > 0.f ? fb * (b.U + db * b.S) : 0.f);
+    r.m = x.m == x.m ? x.m : y.m;
+    r.S = fmaf(f, y.S, x.S);
+    r.U = x.U + (f > 0.f ? f * fmaf(d, y.S, y.U) : 0.f);  // 0 times -infinity (a part 2^200 below the other) must not become NaN
+    if (d != d) r.S = NAN;
     return r;
+}
+
+// One part from those of the 64 lanes.
+__device__ __forceinline__ FieldPart fm_field_wave_merge(FieldPart p)
+{
+    for (int x = 32; x > 0; x >>= 1) p = fm_field_merge(p, {__shfl_xor(p.m, x), __shfl_xor(p.S, x), __shfl_xor(p.U, x)});
+    return p;
 }
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));

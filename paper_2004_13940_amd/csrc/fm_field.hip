@@ -3,9 +3,39 @@
 #include <stdarg.h>
 #include <stdio.h>
 
+#include <atomic>
 #include <new>
 
 #include "fm_field_tiles.h"
+
+namespace {
+// What the runtime said of a kernel, by its address; kernels that find no place are asked about again.
+constexpr size_t KNOWN = 512;
+std::atomic<const void*> known_kernel[KNOWN];
+std::atomic<int> known_resident[KNOWN];
+}  // namespace
+
+int fm_field_resident(const void* kernel, int threads, size_t lds)
+{
+    const size_t at = ((uintptr_t)kernel >> 3) % KNOWN;
+    size_t place = at;
+    for (size_t i = 0; i < KNOWN; ++i, place = (place + 1) % KNOWN) {
+        const void* k = known_kernel[place].load(std::memory_order_acquire);
+        if (k == kernel) {
+            const int n = known_resident[place].load(std::memory_order_acquire);
+            if (n > 0) return n;
+            break;
+        }
+        if (k == nullptr && known_kernel[place].compare_exchange_strong(k, kernel)) break;
+        if (k == kernel) break;
+    }
+    if (lds > FM_FIELD_LDS) (void)hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    int per_cu = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, threads, lds) != hipSuccess) (void)hipGetLastError();
+    const int n = FM_FIELD_CUS * std::max(per_cu, 1);
+    if (known_kernel[place].load() == kernel) known_resident[place].store(n, std::memory_order_release);
+    return n;
+}
 
 namespace {
 
@@ -19,22 +49,24 @@ __device__ __forceinline__ uint32_t logit_key(float z)
 
 __device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float((int32_t)k < 0 ? k & 0x7FFFFFFFu : ~k); }
 
-// Statistics of a row over all splits, the same in all threads of the workgroup.
+// Statistics of a row over all parts of the candidates, the same in all threads of the workgroup.  One wavefront joins them: in
+// the order that k_field_finish has too, so that results do not depend on what else was asked for.
 template <int BS>
 __device__ __forceinline__ FieldPart row_stats(const FieldArgs& A, int64_t row, FieldPart* lds)
 {
     FieldPart p = {-INFINITY, 0.f, 0.f};
-    for (int s = threadIdx.x; s < A.splits; s += BS) {
-        const float4 q = A.part[(int64_t)s * A.n + row];
-        p = fm_field_merge(p, {q.x, q.y, q.z});
+    if (threadIdx.x < 64) {
+#pragma unroll 4
+        for (int s = threadIdx.x; s < A.splits; s += 64) {
+            const float4 q = A.part[(int64_t)s * A.n + row];
+            p = fm_field_merge(p, {q.x, q.y, q.z});
+        }
+        p = fm_field_wave_merge(p);
+        if (BS > 64 && threadIdx.x == 0) *lds = p;
     }
-    for (int x = 32; x > 0; x >>= 1)
-        p = fm_field_merge(p, {__shfl_xor(p.m, x), __shfl_xor(p.S, x), __shfl_xor(p.U, x)});
     if constexpr (BS > 64) {
-        if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = p;
         __syncthreads();
-        p = lds[0];
-        for (int i = 1; i < BS / 64; ++i) p = fm_field_merge(p, lds[i]);
+        p = *lds;
     }
     return p;
 }
@@ -47,29 +79,31 @@ __device__ __forceinline__ uint64_t item_key(float z, float out, uint32_t id)
 }
 __device__ __forceinline__ int64_t key_id(uint64_t key) { return (int64_t)(uint32_t)~(uint32_t)key; }
 
-// The `top` largest keys of `count` items into best[0..top), in order, 0 from where there are no more; item i has value(i) and
-// number(i).  Items go to 64 buckets: what is below the top-th largest of the buckets' maxima is not among the best, and of
-// what is not (a few more than `top`, if the order of the items has nothing to do with the buckets) everyone counts who is
-// before it.  Where that is more than the list holds, the top-th of those in the list is the next bound.  Ends with a barrier.
+// The `top` largest keys of some items into best[0..top), in order, 0 from where there are no more; each(f) calls f(value, number)
+// for every item of the thread.  Items go to 64 buckets: what is below the top-th largest of the buckets' maxima is not
+// among the best, and of what is not (a few more than `top`, if the order of the items has nothing to do with the buckets)
+// everyone counts who is before it.  Where that is more than the list holds, the top-th of those in the list is the next
+// bound.  Ends with a barrier.
 constexpr int SELECT_LIST = 512;
+constexpr int HELD = 12;  // blocks of 64 candidates whose maxima a thread keeps in registers
 template <int BS>
 struct SelectLds {
     uint64_t max[BS], list[SELECT_LIST], from;
     int count;
 };
 
-template <int BS, typename F, typename N>
-__device__ __forceinline__ void select_best(uint32_t count, int top, float out, uint64_t* best, SelectLds<BS>& lds, F value, N number)
+template <int BS, typename E>
+__device__ __forceinline__ void select_best(int top, float out, uint64_t* best, SelectLds<BS>& lds, E each)
 {
     const int tid = threadIdx.x;
     float most = -INFINITY;
     uint32_t where = 0;
-#pragma unroll 4
-    for (uint32_t i = tid; i < count; i += BS) {
-        const float v = value(i);
-        if (v > most) most = v, where = i;
-    }
-    uint64_t mine = tid < count ? item_key(most, out, number(where)) : 0;
+    each([&](float v, uint32_t number) {
+        const bool more = v > most;
+        most = more ? v : most;
+        where = more ? number : where;
+    });
+    uint64_t mine = item_key(most, out, where);
     lds.max[tid] = mine;
     if (tid == 0) lds.count = 0, lds.from = 1;
     for (int a = tid; a < top; a += BS) best[a] = 0;
@@ -88,17 +122,15 @@ __device__ __forceinline__ void select_best(uint32_t count, int top, float out, 
     for (;;) {
         __syncthreads();
         const uint64_t from = lds.from;
-        const float least = from == 1 ? -INFINITY : key_logit((uint32_t)(from >> 32));
-#pragma unroll 4
-        for (uint32_t i = tid; i < count; i += BS) {
-            const float v = value(i);
-            if (v < least) continue;
-            const uint64_t k = item_key(v, out, number(i));
+        const float least = from == 1 ? 0.5f * out : key_logit((uint32_t)(from >> 32));
+        each([&](float v, uint32_t number) {
+            if (v < least) return;
+            const uint64_t k = item_key(v, out, number);
             if (k >= from) {
                 const int at = atomicAdd(&lds.count, 1);
                 if (at < SELECT_LIST) lds.list[at] = k;
             }
-        }
+        });
         __syncthreads();
         const int found = lds.count, held = min(found, SELECT_LIST);
         for (int i = tid; i < held; i += BS) {
@@ -115,31 +147,49 @@ __device__ __forceinline__ void select_best(uint32_t count, int top, float out, 
     }
 }
 
-// What is left of a row: its sums joined, given candidates, best candidates.
-template <typename TV, int BS>
-__global__ __launch_bounds__(BS) void k_field_finish(const FieldArgs A)
+// What is left of a row: its sums joined, given candidates.  16 lanes to a row.
+template <typename TV>
+__global__ __launch_bounds__(FM_BLOCK) void k_field_finish(const FieldArgs A)
 {
-    __shared__ __align__(16) float g[256];
-    __shared__ FieldPart parts[BS / 64];
-    const int tid = threadIdx.x;
-    const int64_t row = blockIdx.x;
-    for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
-    const FieldPart p = row_stats<BS>(A, row, parts);
-    __syncthreads();
+    const int lo = threadIdx.x % 16;
+    const int64_t row = (int64_t)blockIdx.x * (FM_BLOCK / 16) + threadIdx.x / 16;
+    if (row >= A.n) return;
+    FieldPart of[4], p;  // as four of the 64 lanes of row_stats
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        of[i] = {-INFINITY, 0.f, 0.f};
+        for (int s = lo + 16 * i; s < A.splits; s += 64) {
+            const float4 q = A.part[(int64_t)s * A.n + row];
+            of[i] = fm_field_merge(of[i], {q.x, q.y, q.z});
+        }
+    }
+    p = fm_field_merge(fm_field_merge(of[0], of[2]), fm_field_merge(of[1], of[3]));
+    p = fm_field_merge(p, {fm_xor_lane<8>(p.m), fm_xor_lane<8>(p.S), fm_xor_lane<8>(p.U)});
+    p = fm_field_merge(p, {fm_xor_lane<4>(p.m), fm_xor_lane<4>(p.S), fm_xor_lane<4>(p.U)});
+    p = fm_field_merge(p, {fm_xor_lane<2>(p.m), fm_xor_lane<2>(p.S), fm_xor_lane<2>(p.U)});
+    p = fm_field_merge(p, {fm_xor_lane<1>(p.m), fm_xor_lane<1>(p.S), fm_xor_lane<1>(p.U)});
     const bool empty = p.S == 0.f, nan = p.S != p.S;
     const float log2S = __builtin_amdgcn_logf(p.S);
-    if (tid == 0) {
+    if (lo == 0) {
         if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
         if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
     }
-    const auto logprob = [&](float z) {
-        return nan ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
-    };
-    if (A.logprob != nullptr)
-        for (int t = tid; t < A.T; t += BS) {
-            const int64_t j = A.ids[row * A.T + t];
-            A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
+    if (A.logprob == nullptr) return;
+    const float* g = A.G + row * A.g_stride;
+    for (int t = 0; t < A.T; ++t) {
+        const int64_t j = A.ids[row * A.T + t];
+        if (j < 0 || j >= A.C) {
+            if (lo == 0) A.logprob[row * A.T + t] = 0.f;
+            continue;
         }
+        const TV* v = static_cast<const TV*>(A.V) + j * A.v_stride;
+        float z = 0.f;
+        for (int k = lo; k < A.K; k += 16) z = fmaf(g[k], fm_field_value(v + k), z);
+        z = fm_group_sum<16>(z);
+        z = fmaf(z, 0.f, z) + (A.w != nullptr ? A.w[j] : 0.f);
+        if (!fm_field_allowed(A, row, j)) z = -INFINITY;
+        if (lo == 0) A.logprob[row * A.T + t] = nan ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
+    }
 }
 
 // The same with the best candidates: the groups with the `top` largest maxima hold them (lower blocks first among equal
@@ -149,14 +199,14 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
 {
     extern __shared__ __align__(16) float zs[];  // [4 top][16]
     __shared__ __align__(16) float g[256];
-    __shared__ FieldPart parts[BS / 64];
+    __shared__ FieldPart parts;
     __shared__ SelectLds<BS> lds;
     __shared__ uint64_t best[FM_FIELD_TOP];
     __shared__ int32_t groups[4 * FM_FIELD_TOP], ngroups;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
-    const FieldPart p = row_stats<BS>(A, row, parts);
+    const FieldPart p = row_stats<BS>(A, row, &parts);
     __syncthreads();
     const bool empty = p.S == 0.f, nan = p.S != p.S;
     const float log2S = __builtin_amdgcn_logf(p.S);
@@ -173,52 +223,76 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
             const int64_t j = A.ids[row * A.T + t];
             A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
         }
-    // of the parts of the candidates those with the largest maxima, of these the groups, of these the candidates
+    // of the parts of the candidates those with the largest maxima, of these the groups, of these the candidates; where there
+    // are not too many groups, of all of them
     const float* gm = A.gmax + row * A.blocks * 4;
+    const float4* gm4 = reinterpret_cast<const float4*>(gm);
     const uint32_t in_split = (uint32_t)(A.chunk / FM_BLOCK_CANDS * 4), all_groups = (uint32_t)(A.blocks * 4);
-    const bool all = A.splits <= 2 * A.top || all_groups <= 64 * BS;
-    int nsplits = A.splits, ng = 0;
-    const auto group = [&](uint32_t i) {  // i-th group of the parts that were taken
-        return all ? i : (uint32_t)groups[i / in_split] * in_split + i % in_split;
-    };
+    if (nan) {
+        for (int a = tid; a < A.top; a += BS) best[a] = 0;
+        __syncthreads();
+    } else if (A.blocks <= HELD * BS) {
+        float4 held[HELD];
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held[i] = gm4[min(tid + i * BS, (int)A.blocks - 1)];
+        select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
+#pragma unroll
+            for (int i = 0; i < HELD; ++i) {
+                const int b = tid + i * BS;
+                if (b < A.blocks) f(held[i].x, 4 * b), f(held[i].y, 4 * b + 1), f(held[i].z, 4 * b + 2), f(held[i].w, 4 * b + 3);
+            }
+        });
+    } else {
+        const bool all = A.splits <= 2 * A.top;
+        uint32_t nsplits = A.splits;
+        if (!all) {
+            select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
+#pragma unroll 4
+                for (uint32_t i = tid; i < (uint32_t)A.splits; i += BS) f(A.part[(int64_t)i * A.n + row].w, i);
+            });
+            nsplits = 0;
+            for (int a = 0; a < A.top; ++a) nsplits += best[a] != 0;
+            if (tid < (int)nsplits) groups[tid] = (int32_t)key_id(best[tid]);
+            __syncthreads();
+        }
+        const uint32_t quads = in_split / 4;
+        select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
+#pragma unroll 4
+            for (uint32_t i = tid; i < nsplits * quads; i += BS) {
+                const uint32_t b = (all ? i / quads : (uint32_t)groups[i / quads]) * quads + i % quads;
+                if (b >= (uint32_t)A.blocks) continue;
+                const float4 v = gm4[b];
+                f(v.x, 4 * b), f(v.y, 4 * b + 1), f(v.z, 4 * b + 2), f(v.w, 4 * b + 3);
+            }
+        });
+    }
+    for (int i = tid; i < 4 * A.top; i += BS) {
+        const uint64_t k = best[i / 4];
+        if (k == 0) continue;
+        const int64_t id = key_id(k), other = id / 4 * 4 + i % 4;
+        bool take = other == id;
+        if (!take) {  // equal to the last one that was taken, and not taken itself
+            const uint64_t last = best[A.top - 1], mine = item_key(gm[other], A.out, (uint32_t)other);
+            take = last != 0 && mine < last && mine >> 32 == last >> 32;
+            for (int o = 0; take && o < i / 4; ++o) take = best[o] == 0 || key_id(best[o]) / 4 != id / 4;  // once for the block
+        }
+        if (take) groups[atomicAdd(&ngroups, 1)] = (int32_t)other;
+    }
+    __syncthreads();
+    const int ng = ngroups;
     const auto candidate = [&](uint32_t i) {  // i-th candidate of the groups that were taken
         const uint32_t id = (uint32_t)groups[i / 16];
         return id / 4 * FM_BLOCK_CANDS + 4 * (id % 4) + i % 16 / 4 * 16 + i % 4;
     };
-    for (int stage = all ? 1 : 0; stage < 3; ++stage) {
-        const uint32_t count = nan ? 0 : stage == 0 ? A.splits : stage == 2 ? 16 * ng : all ? all_groups : nsplits * in_split;
-        select_best<BS>(count, A.top, A.out, best, lds, [&](uint32_t i) {
-            if (stage == 0) return A.part[(int64_t)i * A.n + row].w;
-            if (stage == 2) return zs[i];
-            const uint32_t at = group(i);
-            return at < all_groups ? gm[at] : -INFINITY;
-        }, [&](uint32_t i) { return stage == 0 ? i : stage == 1 ? group(i) : candidate(i); });
-        if (stage == 0) {
-            nsplits = 0;
-            for (int a = 0; a < A.top; ++a) nsplits += best[a] != 0;
-            if (tid < nsplits) groups[tid] = (int32_t)key_id(best[tid]);
-        } else if (stage == 1) {
-            for (int i = tid; i < 4 * A.top; i += BS) {
-                const uint64_t k = best[i / 4];
-                if (k == 0) continue;
-                const int64_t id = key_id(k), other = id / 4 * 4 + i % 4;
-                bool take = other == id;
-                if (!take) {  // equal to the last one that was taken, and not taken itself
-                    const uint64_t last = best[A.top - 1], mine = item_key(gm[other], A.out, (uint32_t)other);
-                    take = last != 0 && mine < last && mine >> 32 == last >> 32;
-                    for (int o = 0; take && o < i / 4; ++o) take = best[o] == 0 || key_id(best[o]) / 4 != id / 4;  // once for the block
-                }
-                if (take) groups[atomicAdd(&ngroups, 1)] = (int32_t)other;
-            }
-            __syncthreads();
-            ng = ngroups;
-            for (int i = tid; i < 16 * ng; i += BS) {
-                const int64_t j = candidate(i);
-                zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
-            }
-        }
-        __syncthreads();
+    for (int i = tid; i < 16 * ng; i += BS) {
+        const int64_t j = candidate(i);
+        zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
     }
+    __syncthreads();
+    select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
+#pragma unroll 4
+        for (uint32_t i = tid; i < 16u * ng; i += BS) f(zs[i], candidate(i));
+    });
     for (int a = tid; a < A.top; a += BS) {
         const uint64_t k = best[a];
         if (A.top_ids != nullptr) A.top_ids[row * A.top + a] = k == 0 ? -1 : (int32_t)key_id(k);
@@ -234,7 +308,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
     constexpr int KP = 16 * KC;
     extern __shared__ float2 entries[];  // [T] logit and scaled teacher logit, then the share of the entry; behind them [splits] floats
     __shared__ __align__(16) float g[256];
-    __shared__ FieldPart parts[BS / 64];
+    __shared__ FieldPart parts;
     __shared__ float sums[BS / 64], wide[BS];
     float* factor = reinterpret_cast<float*>(entries + A.T);
     const int tid = threadIdx.x;
@@ -269,7 +343,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
         return;
     }
     for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
-    const FieldPart p = row_stats<BS>(A, row, parts);
+    const FieldPart p = row_stats<BS>(A, row, &parts);
     __syncthreads();
     const float log2S = __builtin_amdgcn_logf(p.S);
     const auto block = [&](float x, bool largest) {
@@ -317,7 +391,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
             const float d = (y - log2Q) - (fmaf(e.x, A.sl, -p.m) - log2S);
             if (q != 0.f) x += q * d * FM_LN2;
         }
-        entries[t] = make_float2(q * r, 0.f);
+        entries[t] = make_float2(q * r, __int_as_float(q == 0.f ? 0 : ids[t]));
     }
     x = block(x, false);
     const float rs = counts ? r / p.S : 0.f;
@@ -353,10 +427,13 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
 #pragma unroll 8
             for (int i = slice; i < A.splits; i += slices) s = fmaf(factor[i], o[(int64_t)i * A.n * KP], s);
             s *= rs;
-            for (int t = slice; t < A.T; t += slices) {
-                const float q = entries[t].x;
-                if (q != 0.f && k < A.K) s = fmaf(-q, fm_field_value(V + (int64_t)ids[t] * A.v_stride + k), s);
-            }
+            if (k < A.K)
+#pragma unroll 8
+                for (int t = slice; t < A.T; t += slices) {
+                    const float2 e = entries[t];
+                    const float v = fm_field_value(V + (int64_t)__float_as_int(e.y) * A.v_stride + k);
+                    s = e.x != 0.f ? fmaf(-e.x, v, s) : s;
+                }
         }
         __syncthreads();
         wide[tid] = s;
@@ -417,11 +494,7 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
     });
 }
 
-#ifndef ROWITEMS
-#define ROWITEMS 8192
-#define COLITEMS 8192
-#endif
-constexpr int FIELD_ROW_ITEMS = ROWITEMS, FIELD_COL_ITEMS = COLITEMS;                        // wavefronts that a sweep is split into, at most and if there is as much to do
+constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
 constexpr int64_t FIELD_WIDE_ROWS = 2048;                // below, a row gets a workgroup of four wavefronts, else one
@@ -528,6 +601,25 @@ int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_
     return FM_OK;
 }
 
+// Into how many parts the axis that a sweep runs along is split.  `groups` workgroups take a part, `resident` run at once, so
+// s parts come in r = ceil(groups s / resident) turns of work resident / (groups s) each, and every part costs `part_us` for its
+// sums.  For each r the best s is the largest one, or where the two costs are in balance.
+constexpr double PART_US = 2 / 3e6;  // a byte written and read again, at 3 TB/s
+double field_us(int64_t n, int64_t C, int32_t K) { return (double)n * (double)C * (0.3 + 0.01 * K) * 1e-6; }  // about what a sweep takes
+int64_t split_count(int64_t groups, int64_t resident, int64_t most, double work_us, double part_us)
+{
+    int64_t best = 1;
+    double least = 1e300;
+    const double turn_us = work_us * (double)resident / (double)std::max<int64_t>(groups, 1);
+    for (int r = 1; r <= 6; ++r) {
+        const double balance = sqrt(r * turn_us / std::max(part_us, 1e-9));
+        const int64_t s = std::max<int64_t>(1, std::min({r * resident / std::max<int64_t>(groups, 1), most, (int64_t)std::min(balance, 1e9)}));
+        const double us = (double)up(groups * s, resident) / (double)s * turn_us + (double)s * part_us;
+        if (us < 0.99 * least) least = us, best = s;
+    }
+    return best;
+}
+
 FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
 {
     FieldArgs A = {};
@@ -545,11 +637,13 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.sl = c->scale * FM_LOG2E;
     A.out = -std::min(1e30f, 1e36f / A.sl);
     A.packed = f->packs && n > FIELD_DIRECT_ROWS;
-    const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed);
+    const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed), KP = 16 * fm_field_chunks(f->K);
     A.row_tiles = (int32_t)up(n, per);
-    // straight from V a part of the candidates is shared by the wavefronts of a workgroup
-    const int64_t share = A.packed ? 1 : FM_FIELD_SHARE, blocks = up(f->C, FM_BLOCK_CANDS);
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(FIELD_ROW_ITEMS / share / std::max(A.row_tiles, 1), up(blocks, share)));
+    const FieldGrid rows = fm_field_rows_grid(distill, A.packed, c->v_type, f->K);
+    const int64_t blocks = up(f->C, FM_BLOCK_CANDS), groups = up(A.row_tiles, rows.tiles);
+    // straight from V the wavefronts of a workgroup share a part of the candidates
+    const int64_t share = A.packed ? 1 : rows.waves, most = std::min(FIELD_ITEMS / share / std::max<int64_t>(A.row_tiles, 1), up(blocks, share));
+    const int64_t splits = split_count(groups, rows.resident, most, field_us(n, f->C, f->K), (double)n * (16 + (distill ? 4 * KP : 0)) * PART_US);
     A.chunk = up(blocks, splits) * FM_BLOCK_CANDS;
     A.splits = (int32_t)up(f->C, A.chunk);
     A.blocks = up(f->C, FM_BLOCK_CANDS);
@@ -573,7 +667,9 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.entry_shift = entry_shift(f->C, f->max_rows);
     A.entry_blocks = (int32_t)up(f->C, int64_t(1) << A.entry_shift);
     A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
-    const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(FIELD_COL_ITEMS / A.col_tiles, A.npad / 32));
+    const FieldGrid cols = fm_field_cols_grid(c->v_type, f->K);
+    const int64_t parts = split_count(up(A.col_tiles, cols.tiles), cols.resident, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 32),
+                                      field_us(n, f->C, f->K), (double)f->C * (4 + 4 * KP) * PART_US);
     A.row_chunk = (int32_t)std::max<int64_t>(32, up(up(A.npad, parts), 32) * 32);
     A.row_splits = (int32_t)std::max<int64_t>(1, up(A.npad, A.row_chunk));
     return A;
@@ -618,10 +714,10 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     f->max_top = max_top;
     f->max_entries = max_entries;
     f->packs = max_rows > FIELD_DIRECT_ROWS && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
-    // of n rows in tiles of `per`: at most FIELD_ROW_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
-    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ROW_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
+    // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
+    f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
     const int64_t tiles = up(C, fm_field_cols_per_wave(K));
-    const int64_t col_parts = std::min(FIELD_COL_ITEMS / tiles, whole32(max_rows) / 32);
+    const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole32(max_rows) / 32);
     f->col_parts = col_parts > 1 && max_entries > 0 ? C * col_parts : 0;  // a single part is written to where it belongs
     f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / (4 * up(C, FM_BLOCK_CANDS))));
     const size_t bytes = Layout(f).bytes;
@@ -678,7 +774,7 @@ extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n,
             using TV = std::remove_pointer_t<decltype(t)>;
             const uint32_t rows = (uint32_t)A.n, lds = (uint32_t)top * 4 * 16 * sizeof(float);
             if (top == 0)
-                n < FIELD_WIDE_ROWS ? k_field_finish<TV, FM_BLOCK><<<rows, FM_BLOCK, 0, st>>>(A) : k_field_finish<TV, 64><<<rows, 64, 0, st>>>(A);
+                k_field_finish<TV><<<(rows + FM_BLOCK / 16 - 1) / (FM_BLOCK / 16), FM_BLOCK, 0, st>>>(A);
             else
                 n < FIELD_WIDE_ROWS ? k_field_finish_top<TV, FM_BLOCK><<<rows, FM_BLOCK, lds, st>>>(A) : k_field_finish_top<TV, 64><<<rows, 64, lds, st>>>(A);
         });

@@ -232,15 +232,29 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_cols_sum(const FieldArgs A, 
 
 int fm_field_cols_per_wave(int32_t K) { return 16 * fm_field_col_tiles(fm_field_chunks(K)); }
 
-void fm_field_cols(int32_t v_type, const FieldArgs& A, hipStream_t st)
+template <typename F>
+static void cols_kernel(int32_t v_type, int32_t K, F run)
 {
-    fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto fill) {
+    fm_field_shape(v_type, K, [&](auto type, auto kc, auto fill) {
         using TV = decltype(type);
         constexpr int KC = decltype(kc)::value, W = ColsShape<KC>::W;
         constexpr size_t lds = ColsShape<KC>::STAGED ? 2 * (ColsShape<KC>::template ops<FmParts<TV>::value>() * 64 + 16) * sizeof(u32x4) : 0;
-        const auto kernel = k_field_cols<TV, KC, decltype(fill)::value, fm_field_col_tiles(KC)>;
-        if (lds > 48 * 1024) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-        kernel<<<(uint32_t)((A.col_tiles + W - 1) / W * A.row_splits), 64 * W, lds, st>>>(A);
+        run(k_field_cols<TV, KC, decltype(fill)::value, fm_field_col_tiles(KC)>, W, lds);
+    });
+}
+
+FieldGrid fm_field_cols_grid(int32_t v_type, int32_t K)
+{
+    FieldGrid grid = {};
+    cols_kernel(v_type, K, [&](auto kernel, int waves, size_t lds) { grid = {waves, waves, fm_field_resident((const void*)kernel, 64 * waves, lds)}; });
+    return grid;
+}
+
+void fm_field_cols(int32_t v_type, const FieldArgs& A, hipStream_t st)
+{
+    cols_kernel(v_type, A.K, [&](auto kernel, int waves, size_t lds) {
+        if (lds > FM_FIELD_LDS) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        kernel<<<(uint32_t)((A.col_tiles + waves - 1) / waves * A.row_splits), 64 * waves, lds, st>>>(A);
     });
     if (A.row_splits == 1) return;
     const int KP = 16 * fm_field_chunks(A.K);

@@ -418,26 +418,47 @@ __global__ __launch_bounds__((64 * RowsShape<NP, KC, DISTILL>::W), KC == 16 ? 1 
 
 uint32_t blocks_of(int64_t wavefronts) { return (uint32_t)((wavefronts + FM_WAVES - 1) / FM_WAVES); }
 
+// Calls run(the kernel of the sweep, its shape: wavefronts, bytes of LDS).
+template <bool DISTILL, typename F>
+void rows_kernel(bool packed, int32_t v_type, int32_t K, F run)
+{
+    fm_field_shape(v_type, K, [&](auto type, auto kc, auto fill) {
+        using TV = decltype(type);
+        constexpr int KC = decltype(kc)::value, FILL = decltype(fill)::value;
+        using Shape = RowsShape<FmParts<TV>::value, KC, DISTILL>;
+        constexpr size_t lds = Shape::STAGED ? 2 * (Shape::OPS * 64 + 16) * sizeof(u32x4) : 0;
+        if (packed)
+            run(k_field_rows_packed<FmParts<TV>::value, KC, fm_field_row_tiles(KC, DISTILL), DISTILL>, k_field_pack<TV, KC, FILL, DISTILL>, Shape::W, lds);
+        else
+            run(k_field_rows<TV, KC, FILL, DISTILL>, k_field_pack<TV, KC, FILL, DISTILL>, FM_FIELD_SHARE, (size_t)0);
+    });
+}
+
 template <bool DISTILL>
 void rows(int32_t v_type, const FieldArgs& A, hipStream_t st)
 {
-    fm_field_shape(v_type, A.K, [&](auto type, auto kc, auto fill) {
-        using TV = decltype(type);
-        constexpr int KC = decltype(kc)::value, FILL = decltype(fill)::value;
+    rows_kernel<DISTILL>(A.packed, v_type, A.K, [&](auto kernel, auto pack, int waves, size_t lds) {
         if (A.packed) {
-            k_field_pack<TV, KC, FILL, DISTILL><<<blocks_of(A.blocks * 2), FM_BLOCK, 0, st>>>(A);
-            using Shape = RowsShape<FmParts<TV>::value, KC, DISTILL>;
-            constexpr size_t lds = Shape::STAGED ? 2 * (Shape::OPS * 64 + 16) * sizeof(u32x4) : 0;
-            const auto kernel = k_field_rows_packed<FmParts<TV>::value, KC, fm_field_row_tiles(KC, DISTILL), DISTILL>;
-            if (lds > 48 * 1024) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-            kernel<<<(uint32_t)((A.row_tiles + Shape::W - 1) / Shape::W * A.splits), 64 * Shape::W, lds, st>>>(A);
-        } else {
-            k_field_rows<TV, KC, FILL, DISTILL><<<(uint32_t)(A.row_tiles * A.splits), 64 * FM_FIELD_SHARE, 0, st>>>(A);
+            pack<<<blocks_of(A.blocks * 2), FM_BLOCK, 0, st>>>(A);
+            if (lds > FM_FIELD_LDS) (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
         }
+        const int tiles = A.packed ? waves : 1;
+        kernel<<<(uint32_t)((A.row_tiles + tiles - 1) / tiles * A.splits), 64 * waves, lds, st>>>(A);
     });
 }
 
 }  // namespace
+
+FieldGrid fm_field_rows_grid(bool distill, bool packed, int32_t v_type, int32_t K)
+{
+    FieldGrid grid = {};
+    const auto ask = [&](auto kernel, auto, int waves, size_t lds) { grid = {packed ? waves : 1, waves, fm_field_resident((const void*)kernel, 64 * waves, lds)}; };
+    if (distill)
+        rows_kernel<true>(packed, v_type, K, ask);
+    else
+        rows_kernel<false>(packed, v_type, K, ask);
+    return grid;
+}
 
 int fm_field_rows_per_wave(bool distill, int32_t K, bool packed)
 {

@@ -145,25 +145,14 @@ __device__ __forceinline__ void load4(const T* row, int k, int K, float (&v)[4])
 // Chunks of 16 latent values that the kernels for K have: 1, 2, 4, 8 or 16.
 constexpr int fm_field_chunks(int32_t K) { return K <= 16 ? 1 : K <= 32 ? 2 : K <= 64 ? 4 : K <= 128 ? 8 : 16; }
 // Tiles of 16 rows, or of 16 candidates, that stay in a wavefront's registers: 256 of them are to do.
-#ifndef LPNT1
-#define LPNT1 4
-#define LPNT4 2
-#define DSNT1 2
-#define DSNT4 2
-#define CNT1 4
-#define CNT4 2
-#endif
-constexpr int fm_field_row_tiles(int KC, bool distill) { return distill ? (KC == 1 ? DSNT1 : KC <= 4 ? DSNT4 : 1) : (KC <= 2 ? LPNT1 : KC <= 8 ? LPNT4 : 1); }
-constexpr int fm_field_col_tiles(int KC) { return KC <= 1 ? CNT1 : KC <= 4 ? CNT4 : 1; }
+constexpr int fm_field_row_tiles(int KC, bool distill) { return distill ? (KC <= 4 ? 2 : 1) : KC <= 2 ? 4 : KC <= 4 ? 2 : 1; }
+constexpr int fm_field_col_tiles(int KC) { return KC == 1 ? 4 : KC <= 4 ? 2 : 1; }
 
 // Operands that the wavefronts of a workgroup read in turn, 1 KB each, go through LDS in two stages: of so many operands to a
 // stage, four wavefronts to a workgroup, eight where two workgroups would not fit a compute unit, and straight from the
 // caches where one does not.
-constexpr int fm_field_waves(int ops) { return ops <= 32 ? 4 : 8; }
-#ifndef STAGEMAX
-#define STAGEMAX 64
-#endif
-constexpr bool fm_field_staged(int ops) { return ops <= STAGEMAX; }
+constexpr bool fm_field_staged(int ops) { return ops <= 64; }
+constexpr int fm_field_waves(int ops) { return ops <= 32 || !fm_field_staged(ops) ? 4 : 8; }
 
 // A stage of OPS operands and EXTRA single values of 16 bytes on its way from memory to LDS: asked for while the one before it
 // is worked on, written when that is done.
@@ -222,6 +211,17 @@ void fm_field_shape(int32_t v_type, int32_t K, F run)
         default: return by_k(float{});
     }
 }
+
+// Of a sweep: tiles of rows (or candidates) to a workgroup, wavefronts in it, workgroups that run at once.
+struct FieldGrid {
+    int tiles, waves, resident;
+};
+FieldGrid fm_field_rows_grid(bool distill, bool packed, int32_t v_type, int32_t K);
+FieldGrid fm_field_cols_grid(int32_t v_type, int32_t K);
+constexpr int FM_FIELD_CUS = 256;
+constexpr size_t FM_FIELD_LDS = 28 * 1024;  // above, with what kernels have of their own, the runtime has to be asked for more than 64 KB
+
+int fm_field_resident(const void* kernel, int threads, size_t lds);  // workgroups that run at once
 
 int fm_field_rows_per_wave(bool distill, int32_t K, bool packed);
 void fm_field_rows(bool distill, int32_t v_type, const FieldArgs& A, hipStream_t st);  // through the packed table where A.packed
