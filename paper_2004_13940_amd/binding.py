@@ -333,17 +333,19 @@ class Matrix:
                 for k in range(nk)}
 
 
-def _rows(t, n, K, dtypes, what):
+def _rows(t, n, K, types, what):
     """Row stride of a CUDA tensor of n rows of K values, one after another in a row; a flat one is taken as contiguous."""
-    if not (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype in dtypes):
-        raise TypeError(f"{what} must be a CUDA tensor of type {' or '.join(str(d) for d in dtypes)}")
-    if t.dim() == 1 and t.numel() == n * K and t.is_contiguous():
+    if not (isinstance(t, _torch.Tensor) and t.is_cuda and t.dtype in types):
+        raise TypeError(f"{what} must be a CUDA tensor of type {' or '.join(str(d) for d in types)}")
+    shape = t.shape
+    if len(shape) == 1 and shape[0] == n * K and t.is_contiguous():
         return K
-    if t.dim() != 2 or t.shape[0] != n or t.shape[1] != K:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected ({n}, {K})")
-    if t.numel() and K > 1 and t.stride(1) != 1:
+    if len(shape) != 2 or shape[0] != n or shape[1] != K:
+        raise ValueError(f"{what} has shape {tuple(shape)}, expected ({n}, {K})")
+    row, step = t.stride()
+    if step != 1 and K > 1 and n > 0:
         raise TypeError(f"the values of a row of {what} must be contiguous")
-    return max(K, t.stride(0)) if n <= 1 else t.stride(0)
+    return row if n > 1 else max(K, row)
 
 
 def _out(t, n, dtype, what):
@@ -366,6 +368,7 @@ class Field:
             raise RuntimeError("no GPU: the operators of a field only run on the HIP library")
         lib = load()
         self.C, self.K = int(C), int(K)
+        self._types = {torch.float32: FM_TYPE_F32, torch.float16: FM_TYPE_F16, torch.bfloat16: FM_TYPE_BF16}
         torch.cuda.current_stream()  # the runtime's device is torch's from here on
         self._h = ctypes.c_void_p(None)
         rc = lib.fm_field_create(self.C, self.K, int(max_rows), int(max_top), int(max_entries), ctypes.byref(self._h))
@@ -388,8 +391,8 @@ class Field:
             pass
 
     def _candidates(self, n, V, w, mask, scale):
-        types = {_torch.float32: FM_TYPE_F32, _torch.float16: FM_TYPE_F16, _torch.bfloat16: FM_TYPE_BF16}
-        v_stride = _rows(V, self.C, self.K, tuple(types), "V")
+        types = self._types
+        v_stride = _rows(V, self.C, self.K, types, "V")
         _dev(w, self.C, "w")
         mask_stride = 0
         if mask is not None:

@@ -205,36 +205,31 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
     __shared__ int32_t groups[4 * FM_FIELD_TOP], ngroups;
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
+    // what does not depend on anything first
+    const float* gm = A.gmax + row * A.blocks * 4;
+    const float4* gm4 = reinterpret_cast<const float4*>(gm);
+    const bool hold = A.blocks <= HELD * BS;
+    float4 held[HELD];
+    if (hold)
+#pragma unroll
+        for (int i = 0; i < HELD; ++i) held[i] = gm4[min(tid + i * BS, (int)A.blocks - 1)];
+    const int64_t given = A.logprob != nullptr && tid < A.T ? A.ids[row * A.T + tid] : -1;
     for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
+    if (tid == 0) ngroups = 0;
     const FieldPart p = row_stats<BS>(A, row, &parts);
     __syncthreads();
     const bool empty = p.S == 0.f, nan = p.S != p.S;
     const float log2S = __builtin_amdgcn_logf(p.S);
-    if (tid == 0) {
-        if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
-        if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
-        ngroups = 0;
-    }
     const auto logprob = [&](float z) {
         return nan ? NAN : z == -INFINITY ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
     };
-    if (A.logprob != nullptr)
-        for (int t = tid; t < A.T; t += BS) {
-            const int64_t j = A.ids[row * A.T + t];
-            A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
-        }
     // of the parts of the candidates those with the largest maxima, of these the groups, of these the candidates; where there
     // are not too many groups, of all of them
-    const float* gm = A.gmax + row * A.blocks * 4;
-    const float4* gm4 = reinterpret_cast<const float4*>(gm);
-    const uint32_t in_split = (uint32_t)(A.chunk / FM_BLOCK_CANDS * 4), all_groups = (uint32_t)(A.blocks * 4);
+    const uint32_t in_split = (uint32_t)(A.chunk / FM_BLOCK_CANDS * 4);
     if (nan) {
         for (int a = tid; a < A.top; a += BS) best[a] = 0;
         __syncthreads();
-    } else if (A.blocks <= HELD * BS) {
-        float4 held[HELD];
-#pragma unroll
-        for (int i = 0; i < HELD; ++i) held[i] = gm4[min(tid + i * BS, (int)A.blocks - 1)];
+    } else if (hold) {
         select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
 #pragma unroll
             for (int i = 0; i < HELD; ++i) {
@@ -288,10 +283,83 @@ __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
         const int64_t j = candidate(i);
         zs[i] = j < A.C ? fm_field_logit<TV>(A, row, g, j) : -INFINITY;
     }
+    if (A.logprob != nullptr)
+        for (int t = tid; t < A.T; t += BS) {
+            const int64_t j = t == tid ? given : A.ids[row * A.T + t];
+            A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(fm_field_logit<TV>(A, row, g, j));
+        }
+    if (tid == 0) {
+        if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
+        if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
+    }
     __syncthreads();
     select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
 #pragma unroll 4
         for (uint32_t i = tid; i < 16u * ng; i += BS) f(zs[i], candidate(i));
+    });
+    for (int a = tid; a < A.top; a += BS) {
+        const uint64_t k = best[a];
+        if (A.top_ids != nullptr) A.top_ids[row * A.top + a] = k == 0 ? -1 : (int32_t)key_id(k);
+        if (A.top_logprob != nullptr)
+            A.top_logprob[row * A.top + a] = nan ? NAN : k == 0 ? -INFINITY : logprob(key_logit((uint32_t)(k >> 32)));
+    }
+}
+
+// A whole row at once, its logits in LDS: few candidates and few rows, where kernels after one another are most of the time.
+template <typename TV, int BS>
+__global__ __launch_bounds__(BS) void k_field_small(const FieldArgs A)
+{
+    extern __shared__ __align__(16) float zs[];  // [C]
+    __shared__ __align__(16) float g[256];
+    __shared__ float sums[3][BS / 64];
+    __shared__ SelectLds<BS> lds;
+    __shared__ uint64_t best[FM_FIELD_TOP];
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const int64_t given = A.logprob != nullptr && tid < A.T ? A.ids[row * A.T + tid] : -1;
+    for (int k = tid; k < A.K; k += BS) g[k] = A.G[row * A.g_stride + k];
+    __syncthreads();
+    float most = A.out;
+    for (int j = tid; j < (int)A.C; j += BS) {
+        const float z = fmaxf_or_nan(fm_field_logit<TV>(A, row, g, j), A.out);
+        zs[j] = z;
+        most = fmaxf(most, z);
+    }
+    for (int x = 32; x > 0; x >>= 1) most = fmaxf(most, __shfl_xor(most, x));
+    if (tid % 64 == 0) sums[0][tid / 64] = most;
+    __syncthreads();
+    for (int i = 0; i < BS / 64; ++i) most = fmaxf(most, sums[0][i]);
+    const float m = fmaxf(most, 0.5f * A.out) * A.sl;  // above what is left out
+    FieldPart p = {m, 0.f, 0.f};
+    for (int j = tid; j < (int)A.C; j += BS) {
+        const float x = fmaf(zs[j], A.sl, -m), e = __builtin_amdgcn_exp2f(x);
+        p.S += e;
+        p.U = fmaf(e, x, p.U);
+    }
+    p.S = fm_wave_sum(p.S);
+    p.U = fm_wave_sum(p.U);
+    if (tid % 64 == 0) sums[1][tid / 64] = p.S, sums[2][tid / 64] = p.U;
+    __syncthreads();
+    p.S = p.U = 0.f;
+    for (int i = 0; i < BS / 64; ++i) p.S += sums[1][i], p.U += sums[2][i];
+    const bool empty = p.S == 0.f, nan = p.S != p.S;
+    const float log2S = __builtin_amdgcn_logf(p.S);
+    if (tid == 0) {
+        if (A.lse != nullptr) A.lse[row] = empty ? -INFINITY : (p.m + log2S) * FM_LN2;
+        if (A.entropy != nullptr) A.entropy[row] = empty ? 0.f : (log2S - p.U / p.S) * FM_LN2;
+    }
+    const auto logprob = [&](float z) {
+        return nan ? NAN : z <= 0.5f * A.out ? -INFINITY : (fmaf(z, A.sl, -p.m) - log2S) * FM_LN2;
+    };
+    if (A.logprob != nullptr)
+        for (int t = tid; t < A.T; t += BS) {
+            const int64_t j = t == tid ? given : A.ids[row * A.T + t];
+            A.logprob[row * A.T + t] = j < 0 || j >= A.C ? 0.f : logprob(zs[j]);
+        }
+    if (A.top == 0) return;
+    select_best<BS>(A.top, A.out, best, lds, [&](auto f) {
+        if (nan) return;
+        for (uint32_t j = tid; j < (uint32_t)A.C; j += BS) f(zs[j], j);
     });
     for (int a = tid; a < A.top; a += BS) {
         const uint64_t k = best[a];
@@ -498,6 +566,11 @@ constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sw
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
 constexpr int64_t FIELD_WIDE_ROWS = 2048;                // below, a row gets a workgroup of four wavefronts, else one
+// Logits of a row in LDS, one kernel: V of up to so many values, rows of 16 of them at least, and up to so many rows.  us, one kernel /
+// several: 1 x 1,000 (K = 8) 9.9 / 17.3, 1 x 4,096 (K = 16) 11.7 / 17.4, 1 x 8,192 18.5 / 17.4, 256 x 4,096 14.2 / 21.8,
+// 512 x 1,000 9.9 / 22.2, 512 x 8,000 26.6 / 25.0.
+constexpr int64_t FIELD_SMALL_VALUES = 65536, FIELD_SMALL_ROWS = 512;
+constexpr int FIELD_SMALL_BLOCK = 512;  // threads; 1 x 4,096: 256 threads 16.6 us, 1024 10.3, 512 x 8,000: 32.7 and 33.9
 constexpr int FIELD_MOST_ENTRIES = 4096;                 // of a teacher, to a row
 constexpr int64_t FIELD_STARTS = int64_t(1) << 26;       // starts of blocks in the lists of entries, about
 constexpr int FIELD_ENTRY_BLOCKS = 4096;                 // blocks to a list, at most
@@ -576,9 +649,17 @@ struct Layout {
     }
 };
 
-// Calls with more rows lay the table out first, unless that takes too much room.
+// Calls lay the table out first where they have more rows than that and more products to a sweep, unless it takes too much room.
+// us, straight from V / laid out: logprobs 384 x 20,000 K=16 24 / 30, 1,536 rows 55 / 52; K=64 192 rows 30 / 36, 384 39 / 37;
+// 192 x 200,000 K=16 46 / 49, 384 71 / 63; K=64 bf16 48 rows 46 / 50, 96 61 / 51.  Distillation 768 x 20,000 K=16 58 / 56, K=64
+// 384 rows 76 / 77, 192 x 200,000 K=16 99 / 98.
 constexpr int64_t FIELD_DIRECT_ROWS = 64;
+constexpr double FIELD_DIRECT_PRODUCTS = 5e8;
 constexpr int64_t FIELD_PACK_BYTES = int64_t(1) << 30;
+bool pays_to_pack(int64_t n, int64_t C, int32_t K)
+{
+    return n > FIELD_DIRECT_ROWS && (double)n * (double)C * (16 * fm_field_chunks(K)) > FIELD_DIRECT_PRODUCTS;
+}
 
 int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
 {
@@ -603,18 +684,18 @@ int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_
 
 // Into how many parts the axis that a sweep runs along is split.  `groups` workgroups take a part, `resident` run at once, so
 // s parts come in r = ceil(groups s / resident) turns of work resident / (groups s) each, and every part costs `part_us` for its
-// sums.  For each r the best s is the largest one, or where the two costs are in balance.
+// sums, and several parts a kernel that joins them.  For each r the best s is the largest one, or where the two costs are in balance.
 constexpr double PART_US = 2 / 3e6;  // a byte written and read again, at 3 TB/s
 double field_us(int64_t n, int64_t C, int32_t K) { return (double)n * (double)C * (0.3 + 0.01 * K) * 1e-6; }  // about what a sweep takes
-int64_t split_count(int64_t groups, int64_t resident, int64_t most, double work_us, double part_us)
+int64_t split_count(int64_t groups, int64_t resident, int64_t most, double work_us, double part_us, double join_us)
 {
     int64_t best = 1;
     double least = 1e300;
     const double turn_us = work_us * (double)resident / (double)std::max<int64_t>(groups, 1);
-    for (int r = 1; r <= 6; ++r) {
+    for (int r = 0; r <= 6; ++r) {  // 0: one part
         const double balance = sqrt(r * turn_us / std::max(part_us, 1e-9));
-        const int64_t s = std::max<int64_t>(1, std::min({r * resident / std::max<int64_t>(groups, 1), most, (int64_t)std::min(balance, 1e9)}));
-        const double us = (double)up(groups * s, resident) / (double)s * turn_us + (double)s * part_us;
+        const int64_t s = r == 0 ? 1 : std::max<int64_t>(1, std::min({r * resident / std::max<int64_t>(groups, 1), most, (int64_t)std::min(balance, 1e9)}));
+        const double us = (double)up(groups * s, resident) / (double)s * turn_us + (double)s * part_us + (s > 1 ? join_us : 0.);
         if (us < 0.99 * least) least = us, best = s;
     }
     return best;
@@ -636,14 +717,14 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.scale = c->scale;
     A.sl = c->scale * FM_LOG2E;
     A.out = -std::min(1e30f, 1e36f / A.sl);
-    A.packed = f->packs && n > FIELD_DIRECT_ROWS;
+    A.packed = f->packs && pays_to_pack(n, f->C, f->K);
     const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed), KP = 16 * fm_field_chunks(f->K);
     A.row_tiles = (int32_t)up(n, per);
     const FieldGrid rows = fm_field_rows_grid(distill, A.packed, c->v_type, f->K);
     const int64_t blocks = up(f->C, FM_BLOCK_CANDS), groups = up(A.row_tiles, rows.tiles);
     // straight from V the wavefronts of a workgroup share a part of the candidates
     const int64_t share = A.packed ? 1 : rows.waves, most = std::min(FIELD_ITEMS / share / std::max<int64_t>(A.row_tiles, 1), up(blocks, share));
-    const int64_t splits = split_count(groups, rows.resident, most, field_us(n, f->C, f->K), (double)n * (16 + (distill ? 4 * KP : 0)) * PART_US);
+    const int64_t splits = split_count(groups, rows.resident, most, field_us(n, f->C, f->K), (double)n * (16 + (distill ? 4 * KP : 0)) * PART_US, 0.);
     A.chunk = up(blocks, splits) * FM_BLOCK_CANDS;
     A.splits = (int32_t)up(f->C, A.chunk);
     A.blocks = up(f->C, FM_BLOCK_CANDS);
@@ -669,7 +750,7 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
     const FieldGrid cols = fm_field_cols_grid(c->v_type, f->K);
     const int64_t parts = split_count(up(A.col_tiles, cols.tiles), cols.resident, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 32),
-                                      field_us(n, f->C, f->K), (double)f->C * (4 + 4 * KP) * PART_US);
+                                      field_us(n, f->C, f->K), (double)f->C * (4 + 4 * KP) * PART_US, 3.);
     A.row_chunk = (int32_t)std::max<int64_t>(32, up(up(A.npad, parts), 32) * 32);
     A.row_splits = (int32_t)std::max<int64_t>(1, up(A.npad, A.row_chunk));
     return A;
@@ -713,7 +794,7 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     f->max_rows = max_rows;
     f->max_top = max_top;
     f->max_entries = max_entries;
-    f->packs = max_rows > FIELD_DIRECT_ROWS && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
+    f->packs = pays_to_pack(max_rows, C, K) && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
     // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
     f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
     const int64_t tiles = up(C, fm_field_cols_per_wave(K));
@@ -769,6 +850,12 @@ extern "C" int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n,
         A.top_ids = top_ids != nullptr ? top_ids + at * top : nullptr;
         A.top_logprob = top_logprob != nullptr ? top_logprob + at * top : nullptr;
         if (top == 0) A.gmax = nullptr;
+        if (f->C * std::max(f->K, 16) <= FIELD_SMALL_VALUES && n <= FIELD_SMALL_ROWS) {
+            by_type(c->v_type, [&](auto* t) {
+                k_field_small<std::remove_pointer_t<decltype(t)>, FIELD_SMALL_BLOCK><<<(uint32_t)n, FIELD_SMALL_BLOCK, (size_t)f->C * sizeof(float), st>>>(A);
+            });
+            return launched(f);
+        }
         fm_field_rows(false, c->v_type, A, st);
         by_type(c->v_type, [&](auto* t) {
             using TV = std::remove_pointer_t<decltype(t)>;

@@ -140,6 +140,28 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
     const int64_t beg = split * A.chunk, end = min(A.C, beg + A.chunk);
     const TV* V = static_cast<const TV*>(A.V);
 
+    // V and w of a tile of 16 candidates; asked for a block of four tiles ahead where there are registers for it
+    constexpr bool AHEAD = KC <= 2;
+    Quad<TV, FILL> quads[AHEAD ? 4 : 1][KC];
+    f32x4 weights[AHEAD ? 4 : 1];
+    const auto ask = [&](int64_t j0, int i, int at) {
+        const bool whole = j0 + FM_BLOCK_CANDS <= A.C;  // the same in all lanes
+        const TV* row = V + (whole ? j0 + 16 * i + lo : min(j0 + 16 * i + lo, A.C - 1)) * A.v_stride;
+#pragma unroll
+        for (int c = 0; c < KC; ++c) quads[at][c].ask(row, 16 * c + 4 * g, A.K);
+        weights[at] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (A.w == nullptr) return;
+        const int64_t j = j0 + 16 * i + 4 * g;
+        if (whole)
+            weights[at] = *reinterpret_cast<const FmUnaligned4<float>::type*>(A.w + j);
+        else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) weights[at][r] = A.w[min(j + r, A.C - 1)];
+    };
+    const int64_t first = beg + wave * FM_BLOCK_CANDS;
+    if (AHEAD && first < end)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ask(first, i, AHEAD ? i : 0);
     float b[NT][KC][4];
     int64_t mask_row[NT];
 #pragma unroll
@@ -153,30 +175,30 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
         }
     }
     RowStats<KC, NT, DISTILL> s(A);
-    for (int64_t j0 = beg + wave * FM_BLOCK_CANDS; j0 < end; j0 += W * FM_BLOCK_CANDS) {
+    for (int64_t j0 = first; j0 < end; j0 += W * FM_BLOCK_CANDS) {
         f32x4 z[4][NT];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float a[KC][4];
-            const TV* v = V + min(j0 + 16 * i + lo, A.C - 1) * A.v_stride;
+            const int at = AHEAD ? i : 0;
+            if (!AHEAD) ask(j0, i, 0);
+            f32x4 w;
 #pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                load4<TV, FILL>(v, 16 * c + 4 * g, A.K, a[c]);
-                finite_or_nan(a[c]);
-            }
-            f32x4 w = {0.f, 0.f, 0.f, 0.f};
-            if (A.w != nullptr)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) w[r] = fmaxf_or_nan(A.w[min(j0 + 16 * i + 4 * g + r, A.C - 1)], A.out);
+            for (int r = 0; r < 4; ++r) w[r] = fmaxf_or_nan(weights[at][r], A.out);
 #pragma unroll
             for (int t = 0; t < NT; ++t) z[i][t] = w;
 #pragma unroll
-            for (int c = 0; c < KC; ++c)
+            for (int c = 0; c < KC; ++c) {
+                float a[4];
+                quads[at][c].get(16 * c + 4 * g, A.K, a);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) z[i][t] = mfma4(a[c][e], b[t][c][e], z[i][t]);
+                    for (int t = 0; t < NT; ++t) z[i][t] = mfma4(a[e], b[t][c][e], z[i][t]);
+            }
         }
+        if (AHEAD && j0 + W * FM_BLOCK_CANDS < end)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) ask(j0 + W * FM_BLOCK_CANDS, i, AHEAD ? i : 0);
         if (A.mask != nullptr || j0 + FM_BLOCK_CANDS > end) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -340,7 +362,10 @@ __global__ __launch_bounds__((64 * RowsShape<NP, KC, DISTILL>::W), KC == 16 ? 1 
 #pragma unroll
         for (int c = 0; c < KC; ++c) {
             float x[4];
-            load4<float, FILL_ANY>(A.G + row * A.g_stride, 16 * c + 4 * g, A.K, x);
+            if (A.K % 4 == 0)
+                load4<float, FILL_QUADS>(A.G + row * A.g_stride, 16 * c + 4 * g, A.K, x);
+            else
+                load4<float, FILL_ANY>(A.G + row * A.g_stride, 16 * c + 4 * g, A.K, x);
             finite_or_nan(x);
             split<3>(f32x4{x[0], x[1], x[2], x[3]}, p[c]);
         }

@@ -142,6 +142,27 @@ __device__ __forceinline__ void load4(const T* row, int k, int K, float (&v)[4])
     }
 }
 
+// Values k..k+3 of a row as they come from memory: what is asked of them later does not wait for the next request.
+template <typename T, int FILL>
+struct Quad {
+    typename FmUnaligned4<T>::type x;
+    __device__ __forceinline__ void ask(const T* row, int k, int K)
+    {
+        if constexpr (FILL == FILL_ANY) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = k + e < K ? row[k + e] : (T)0.f;
+        } else {
+            x = *reinterpret_cast<const typename FmUnaligned4<T>::type*>(row + (FILL == FILL_WHOLE || k < K ? k : 0));
+        }
+    }
+    __device__ __forceinline__ void get(int k, int K, float (&v)[4]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = FILL != FILL_QUADS || k < K ? (float)x[e] : 0.f;
+        finite_or_nan(v);
+    }
+};
+
 // Chunks of 16 latent values that the kernels for K have: 1, 2, 4, 8 or 16.
 constexpr int fm_field_chunks(int32_t K) { return K <= 16 ? 1 : K <= 32 ? 2 : K <= 64 ? 4 : K <= 128 ? 8 : 16; }
 // Tiles of 16 rows, or of 16 candidates, that stay in a wavefront's registers: 256 of them are to do.
