@@ -654,11 +654,12 @@ struct Layout {
 // 192 x 200,000 K=16 46 / 49, 384 71 / 63; K=64 bf16 48 rows 46 / 50, 96 61 / 51.  Distillation 768 x 20,000 K=16 58 / 56, K=64
 // 384 rows 76 / 77, 192 x 200,000 K=16 99 / 98.
 constexpr int64_t FIELD_DIRECT_ROWS = 64;
-constexpr double FIELD_DIRECT_PRODUCTS = 5e8;
+constexpr double FIELD_DIRECT_PRODUCTS = 5e8, FIELD_DIRECT_DISTILL = 2.5e8;
 constexpr int64_t FIELD_PACK_BYTES = int64_t(1) << 30;
-bool pays_to_pack(int64_t n, int64_t C, int32_t K)
+bool pays_to_pack(bool distill, int64_t n, int64_t C, int32_t K)
 {
-    return n > FIELD_DIRECT_ROWS && (double)n * (double)C * (16 * fm_field_chunks(K)) > FIELD_DIRECT_PRODUCTS;
+    const double products = (double)n * (double)C * (16 * fm_field_chunks(K));
+    return n > FIELD_DIRECT_ROWS && products > (distill ? FIELD_DIRECT_DISTILL : FIELD_DIRECT_PRODUCTS);
 }
 
 int check(fm_field* f, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
@@ -701,6 +702,13 @@ int64_t split_count(int64_t groups, int64_t resident, int64_t most, double work_
     return best;
 }
 
+// Parts of the rows at most: eight at least, if their sums take no more than half a gigabyte, else by the wavefronts.
+int64_t most_col_parts(int64_t C, int32_t K, int64_t n)
+{
+    const int64_t tiles = up(C, fm_field_cols_per_wave(K)), bytes = C * (16 * fm_field_chunks(K) + 1) * 4;
+    return std::max<int64_t>(1, std::min({std::max<int64_t>(FIELD_ITEMS / tiles, 8), whole32(n) / 32, (int64_t(1) << 29) / bytes}));
+}
+
 FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int64_t n, const float* G, int64_t g_stride)
 {
     FieldArgs A = {};
@@ -717,7 +725,7 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.scale = c->scale;
     A.sl = c->scale * FM_LOG2E;
     A.out = -std::min(1e30f, 1e36f / A.sl);
-    A.packed = f->packs && pays_to_pack(n, f->C, f->K);
+    A.packed = f->packs && pays_to_pack(distill, n, f->C, f->K);
     const int64_t per = fm_field_rows_per_wave(distill, f->K, A.packed), KP = 16 * fm_field_chunks(f->K);
     A.row_tiles = (int32_t)up(n, per);
     const FieldGrid rows = fm_field_rows_grid(distill, A.packed, c->v_type, f->K);
@@ -749,7 +757,7 @@ FieldArgs arguments(const fm_field* f, bool distill, const fm_candidates* c, int
     A.entry_blocks = (int32_t)up(f->C, int64_t(1) << A.entry_shift);
     A.col_tiles = (int32_t)up(f->C, fm_field_cols_per_wave(f->K));
     const FieldGrid cols = fm_field_cols_grid(c->v_type, f->K);
-    const int64_t parts = split_count(up(A.col_tiles, cols.tiles), cols.resident, std::min<int64_t>(FIELD_ITEMS / A.col_tiles, A.npad / 32),
+    const int64_t parts = split_count(up(A.col_tiles, cols.tiles), cols.resident, most_col_parts(f->C, f->K, n),
                                       field_us(n, f->C, f->K), (double)f->C * (4 + 4 * KP) * PART_US, 3.);
     A.row_chunk = (int32_t)std::max<int64_t>(32, up(up(A.npad, parts), 32) * 32);
     A.row_splits = (int32_t)std::max<int64_t>(1, up(A.npad, A.row_chunk));
@@ -794,11 +802,10 @@ extern "C" int fm_field_create(int64_t C, int32_t K, int64_t max_rows, int32_t m
     f->max_rows = max_rows;
     f->max_top = max_top;
     f->max_entries = max_entries;
-    f->packs = pays_to_pack(max_rows, C, K) && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
+    f->packs = pays_to_pack(max_entries > 0, max_rows, C, K) && fm_field_pack_bytes(max_entries > 0, K, C) <= FIELD_PACK_BYTES;
     // of n rows in tiles of `per`: at most FIELD_ITEMS / ceil(n / per) parts each, and no more than groups of candidates
     f->slots = std::min(std::max(max_rows, int64_t(FIELD_ITEMS) * fm_field_rows_per_wave(false, K, true)), max_rows * up(C, FM_BLOCK_CANDS));
-    const int64_t tiles = up(C, fm_field_cols_per_wave(K));
-    const int64_t col_parts = std::min(FIELD_ITEMS / tiles, whole32(max_rows) / 32);
+    const int64_t col_parts = most_col_parts(C, K, max_rows);
     f->col_parts = col_parts > 1 && max_entries > 0 ? C * col_parts : 0;  // a single part is written to where it belongs
     f->top_rows = max_top == 0 ? 0 : std::max<int64_t>(1, std::min(max_rows, FIELD_GMAX_FLOATS / (4 * up(C, FM_BLOCK_CANDS))));
     const size_t bytes = Layout(f).bytes;

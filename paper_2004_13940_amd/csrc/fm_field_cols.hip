@@ -77,16 +77,26 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
     const int64_t last_word = row_masks ? ((A.C - 1) >> 5) - (c0 >> 5) : 0;
     const uint32_t* starts = A.starts + (c0 >> A.entry_shift);
     const uint32_t in_block = (uint32_t)(c0 & ((int64_t(1) << A.entry_shift) - 1));
-    // the entries of a tile of rows, the same range in all lanes, and the first 64 of them: asked for a tile ahead
-    uint32_t from_next = 0, to_next = 0;
-    uint2 entry_next = make_uint2(0, 0);
-    const auto named = [&](int i0) {
-        const uint32_t* range = starts + (int64_t)(i0 / 32) * (A.entry_blocks + 1);
-        from_next = __builtin_amdgcn_readfirstlane(range[0]);
-        to_next = idle ? from_next : __builtin_amdgcn_readfirstlane(range[1]);
-        if (from_next + lane < to_next) entry_next = A.entries[(int64_t)i0 * A.T + from_next + lane];
+    // the range of a tile's entries is asked for two tiles ahead (by scalar loads: it is the same in all lanes), the first 64 of
+    // them one ahead
+    struct Range {
+        uint32_t from, to;
     };
-    if (beg < end) named(beg);
+    const auto range_of = [&](int i0) {
+        typedef const __attribute__((address_space(4))) uint32_t* Constant;
+        const Constant r = (Constant)(uintptr_t)(starts + (int64_t)((i0 < end ? i0 : beg) / 32) * (A.entry_blocks + 1));
+        return Range{r[0], idle ? r[0] : r[1]};
+    };
+    Range named = {0, 0}, named_next = {0, 0};
+    uint2 entry = make_uint2(0, 0);
+    const auto first_entries = [&](int i0) {
+        if (named.from + lane < named.to) entry = A.entries[(int64_t)i0 * A.T + named.from + lane];
+    };
+    if (beg < end) {
+        named = range_of(beg);
+        named_next = range_of(beg + 32);
+        first_entries(beg);
+    }
     if (STAGED && beg < end) {
         next.put(stages);
         __syncthreads();
@@ -97,11 +107,9 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
         const u32x4* gs = STAGED ? ops + 2 * Ops::NG * 64 : A.gs + (int64_t)(i0 / 32) * KC * 3 * 64;
         const f32x4* ms = STAGED ? reinterpret_cast<const f32x4*>(ops + OPS * 64) : reinterpret_cast<const f32x4*>(A.rms) + i0 / 32 * 16;
         if (STAGED && i0 + 32 < end) ask(i0 + 32);
-        const uint2* entries = A.entries + (int64_t)i0 * A.T;
-        const uint32_t from = from_next, to = to_next;
-        const uint2 entry = entry_next;
-        named(i0 + 32 < end ? i0 + 32 : i0);
+        const uint32_t from = named.from, to = named.to;
         if (from != to) {
+            const uint2* entries = A.entries + (int64_t)i0 * A.T;
             for (uint32_t i = from + lane; i < to; i += 64) {
                 const uint2 e = i < from + 64 ? entry : entries[i];
                 const uint32_t j = (e.x >> 5) - in_block;
@@ -109,6 +117,9 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
             }
             wave_sync();
         }
+        named = named_next;
+        if (i0 + 32 < end) first_entries(i0 + 32);
+        named_next = range_of(i0 + 64);
         uint32_t words[2][4][(NT + 1) / 2];
         if (row_masks)
 #pragma unroll

@@ -463,3 +463,67 @@ def test_refusals():
         assert entry(**kw) == B.FM_EINVAL, kw
     assert b"mask_stride" in lib.fm_field_last_error(f._h) or lib.fm_field_last_error(f._h)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("n,C,K,T,vtype,mask", [
+    (1700, 20_011, 16, 7, "float32", "rows"), (1700, 20_011, 16, 7, "float16", "shared"), (300, 30_001, 64, 33, "bfloat16", "rows"),
+    (330, 12_345, 100, 5, "float32", "none"), (230, 9_000, 200, 5, "float32", "rows"), (230, 9_001, 256, 5, "bfloat16", "none"),
+    (1700, 9_999, 20, 10, "float16", "rows"), (3000, 5_003, 33, 1, "float32", "shared")])
+def test_from_the_packed_table(n, C, K, T, vtype, mask):
+    """Calls with so many products that the table is laid out first, at every number of chunks and parts."""
+    print("packed", n, C, K, T, vtype, mask, flush=True)
+    d = _data(n + C, n, C, K, T, vtype, mask, True)
+    _check_logprobs(_run_logprobs(d, 1.0, 9), d, 1.0, 9)
+    d = _data(n + C, n, C, K, T, vtype, mask, False)
+    _check_logprobs(_run_logprobs(d, 0.6, 0), d, 0.6, 0)
+    _check_distill(_run_distill(d, 0.6), d, 0.6)
+
+
+def test_every_row_names_the_same_candidates():
+    """More entries in a block of candidates than lanes, and all of them at the same few candidates."""
+    d = _data(31, 500, 9_000, 16, 40, "float32", "none", False)
+    d["ids"] = np.tile(np.arange(40, dtype=np.int32), (500, 1))
+    d["ids"][::3] += 8_950
+    _check_distill(_run_distill(d, 0.7), d, 0.7)
+
+
+@pytest.mark.parametrize("n,C", [(1, 300_000), (20, 300_000), (2100, 20_000)])
+def test_equal_logits_go_to_the_lowest_numbers(n, C):
+    """All logits equal, or equal in long runs: the best are the first ones."""
+    torch = _torch()
+    K = 4
+    f = _field(C, K, n, 20)
+    V, G = torch.ones(C, K, device="cuda"), torch.ones(n, K, device="cuda")
+    ids = torch.empty(n, 20, dtype=torch.int32, device="cuda")
+    f.fm_field_logprobs(G, V, top_ids=ids)
+    assert (ids.cpu() == torch.arange(20)).all()
+    w = torch.zeros(C, device="cuda")
+    w[C // 2 + 3:] = 1.0
+    f.fm_field_logprobs(G, V, w=w, top_ids=ids)
+    assert (ids.cpu() == C // 2 + 3 + torch.arange(20)).all()
+    w[C - 7] = 2.0
+    f.fm_field_logprobs(G, V, w=w, top_ids=ids)
+    assert (ids.cpu()[:, 0] == C - 7).all() and (ids.cpu()[:, 1:] == C // 2 + 3 + torch.arange(19)).all()
+
+
+def test_handles_without_distillation_and_too_many_entries():
+    from paper_2004_13940_amd import binding as B
+    torch = _torch()
+    f = B.Field(100, 8, 10, max_entries=0)
+    G, V = torch.zeros(10, 8, device="cuda"), torch.zeros(100, 8, device="cuda")
+    lse = torch.empty(10, device="cuda")
+    f.fm_field_logprobs(G, V, lse=lse)
+    assert abs(lse.cpu().numpy() - np.log(100)).max() < 1e-5
+    ids, teacher = torch.zeros(10, 2, dtype=torch.int32, device="cuda"), torch.zeros(10, 2, device="cuda")
+    for h in (f, B.Field(100, 8, 10, max_entries=1)):
+        with pytest.raises(B.FMError):
+            h.fm_field_distill(G, V, ids, teacher)
+    B.Field(100, 8, 10, max_entries=2).fm_field_distill(G, V, ids, teacher)
+    torch.cuda.synchronize()
+
+
+def test_a_model_of_a_field_learns_from_its_teacher():
+    from paper_2004_13940_amd import next_item
+    losses, hit = next_item.run(N=3_000, held_out=500, fields=6, width=100, C=600, K=8, T=8, steps=40, eta=5.0)
+    assert np.isfinite(losses).all() and losses[-1] < 0.95 * losses[0]
+    assert hit > 3 * 10 / 600  # three times what ten items drawn at random would have
