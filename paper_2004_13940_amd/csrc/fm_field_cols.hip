@@ -77,24 +77,22 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
     const int64_t last_word = row_masks ? ((A.C - 1) >> 5) - (c0 >> 5) : 0;
     const uint32_t* starts = A.starts + (c0 >> A.entry_shift);
     const uint32_t in_block = (uint32_t)(c0 & ((int64_t(1) << A.entry_shift) - 1));
-    // the range of a tile's entries is asked for two tiles ahead (by scalar loads: it is the same in all lanes), the first 64 of
-    // them one ahead
-    struct Range {
-        uint32_t from, to;
-    };
+    // the range of a tile's entries (the same in all lanes) is asked for two tiles ahead, the first 64 of them one ahead: by vector
+    // loads, whose order lets the waits for LDS pass
     const auto range_of = [&](int i0) {
-        typedef const __attribute__((address_space(4))) uint32_t* Constant;
-        const Constant r = (Constant)(uintptr_t)(starts + (int64_t)((i0 < end ? i0 : beg) / 32) * (A.entry_blocks + 1));
-        return Range{r[0], idle ? r[0] : r[1]};
+        const uint32_t* r = starts + (int64_t)((i0 < end ? i0 : beg) / 32) * (A.entry_blocks + 1);
+        return make_uint2(r[0], r[1]);
     };
-    Range named = {0, 0}, named_next = {0, 0};
-    uint2 entry = make_uint2(0, 0);
+    uint32_t from = 0, to = 0;
+    uint2 entry = make_uint2(0, 0), range = make_uint2(0, 0);
     const auto first_entries = [&](int i0) {
-        if (named.from + lane < named.to) entry = A.entries[(int64_t)i0 * A.T + named.from + lane];
+        from = __builtin_amdgcn_readfirstlane(range.x);
+        to = idle ? from : __builtin_amdgcn_readfirstlane(range.y);
+        if (from + lane < to) entry = A.entries[(int64_t)i0 * A.T + from + lane];
+        range = range_of(i0 + 32);
     };
     if (beg < end) {
-        named = range_of(beg);
-        named_next = range_of(beg + 32);
+        range = range_of(beg);
         first_entries(beg);
     }
     if (STAGED && beg < end) {
@@ -107,8 +105,8 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
         const u32x4* gs = STAGED ? ops + 2 * Ops::NG * 64 : A.gs + (int64_t)(i0 / 32) * KC * 3 * 64;
         const f32x4* ms = STAGED ? reinterpret_cast<const f32x4*>(ops + OPS * 64) : reinterpret_cast<const f32x4*>(A.rms) + i0 / 32 * 16;
         if (STAGED && i0 + 32 < end) ask(i0 + 32);
-        const uint32_t from = named.from, to = named.to;
-        if (from != to) {
+        const bool named = from != to;
+        if (named) {
             const uint2* entries = A.entries + (int64_t)i0 * A.T;
             for (uint32_t i = from + lane; i < to; i += 64) {
                 const uint2 e = i < from + 64 ? entry : entries[i];
@@ -117,9 +115,7 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
             }
             wave_sync();
         }
-        named = named_next;
         if (i0 + 32 < end) first_entries(i0 + 32);
-        named_next = range_of(i0 + 64);
         uint32_t words[2][4][(NT + 1) / 2];
         if (row_masks)
 #pragma unroll
@@ -152,7 +148,7 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
 #pragma unroll
                 for (int r = 0; r < 4; ++r) z[h][t][r] = __builtin_amdgcn_exp2f(fmaf(z[h][t][r], A.sl, -m[r]));
         }
-        if (from != to) {
+        if (named) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
