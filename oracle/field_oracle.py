@@ -48,7 +48,9 @@ def logprobs(z, scale=1.0, ids=None, top=0):
             if np.isnan(lse[i]):
                 out["top_logprob"][i] = np.nan
                 continue
-            best = [j for j in np.lexsort((np.arange(C), -z[i])) if z[i, j] > -np.inf][:top]
+            least = np.partition(z[i], C - top)[C - top] if top < C else -np.inf
+            best = [j for j in np.flatnonzero(z[i] >= least) if z[i, j] > -np.inf]
+            best = sorted(best, key=lambda j: (-z[i, j], j))[:top]
             out["top_ids"][i, :len(best)] = best
             out["top_logprob"][i, :len(best)] = logp[i, best]
     return out

@@ -95,6 +95,8 @@ __device__ __forceinline__ bool fm_field_allowed(const FieldArgs& A, int64_t row
     return A.mask == nullptr || (A.mask[row * A.mask_stride + (j >> 5)] >> (j & 31) & 1u) != 0;
 }
 
+typedef _Float16 fm_f16x8 __attribute__((ext_vector_type(8), aligned(2)));
+typedef __bf16 fm_bf16x8 __attribute__((ext_vector_type(8), aligned(2)));
 template <typename T> struct FmUnaligned4;
 template <> struct FmUnaligned4<float> { typedef float type __attribute__((ext_vector_type(4), aligned(4))); };
 template <> struct FmUnaligned4<_Float16> { typedef _Float16 type __attribute__((ext_vector_type(4), aligned(2))); };
@@ -108,13 +110,27 @@ __device__ __forceinline__ float fm_field_logit(const FieldArgs& A, int64_t row,
     const TV* v = static_cast<const TV*>(A.V) + j * A.v_stride;
     float z = 0.f;
     int k = 0;
-    for (; k + 4 <= A.K; k += 4) {
-        const auto x = *reinterpret_cast<const typename FmUnaligned4<TV>::type*>(v + k);
+    const auto four = [&](float a, float b, float c, float d) {
         const float4 y = *reinterpret_cast<const float4*>(g + k);
-        z = fmaf(y.x, (float)x[0], z);
-        z = fmaf(y.y, (float)x[1], z);
-        z = fmaf(y.z, (float)x[2], z);
-        z = fmaf(y.w, (float)x[3], z);
+        z = fmaf(y.x, a, z);
+        z = fmaf(y.y, b, z);
+        z = fmaf(y.z, c, z);
+        z = fmaf(y.w, d, z);
+        k += 4;
+    };
+    if constexpr (sizeof(TV) == 2) {
+        using Eight = std::conditional_t<std::is_same_v<TV, _Float16>, fm_f16x8, fm_bf16x8>;
+#pragma unroll 4
+        while (k + 8 <= A.K) {
+            const Eight x = *reinterpret_cast<const Eight*>(v + k);
+            four((float)x[0], (float)x[1], (float)x[2], (float)x[3]);
+            four((float)x[4], (float)x[5], (float)x[6], (float)x[7]);
+        }
+    }
+#pragma unroll 4
+    while (k + 4 <= A.K) {
+        const auto x = *reinterpret_cast<const typename FmUnaligned4<TV>::type*>(v + k);
+        four((float)x[0], (float)x[1], (float)x[2], (float)x[3]);
     }
     for (; k < A.K; ++k) z = fmaf(g[k], fm_field_value(v + k), z);
     return fmaf(z, 0.f, z) + (A.w != nullptr ? A.w[j] : 0.f);  // infinite values of G and V count as NaN
