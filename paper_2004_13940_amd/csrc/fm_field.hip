@@ -147,7 +147,8 @@ __device__ __forceinline__ void select_best(int top, float out, uint64_t* best, 
     }
 }
 
-// What is left of a row: its sums joined, given candidates.  16 lanes to a row.
+// What is left of a row: its sums joined, given candidates.  16 lanes to a row: 50,000 rows of five parts 7.5 us, 28 with a wavefront
+// to each.
 template <typename TV>
 __global__ __launch_bounds__(FM_BLOCK) void k_field_finish(const FieldArgs A)
 {
@@ -194,6 +195,10 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_finish(const FieldArgs A)
 
 // The same with the best candidates: the groups with the `top` largest maxima hold them (lower blocks first among equal
 // ones, all groups of a block that are equal to the last), and the logits of these groups are computed once more.
+// Few rows: one chain of loads, barriers and selections, 13 us (64 rows of 602 blocks), of which starting and the sums take 4, the groups 5,
+// their logits 3, the last selection 2.  Many rows: 8,191 of 602 blocks 61 to 75 us, of which the maxima (79 MB) take about 25, the
+// logits of ten groups (168 MB of rows of V from the L2) as long.  Groups of 64 would be a quarter of the maxima and four times the
+// logits; a list that a lane inserts into as it goes would take the registers of the sweep.
 template <typename TV, int BS>
 __global__ __launch_bounds__(BS) void k_field_finish_top(const FieldArgs A)
 {
@@ -370,6 +375,8 @@ __global__ __launch_bounds__(BS) void k_field_small(const FieldArgs A)
 }
 
 // Row i: loss, its gradient by G, and what the candidates need of it.  Rows beyond n, up to a whole tile, are empty ones.
+// Bound by the latency of its chain (sums, ids, the entries' rows of V, parts of the gradient): 16,384 rows of 32 entries 26 us, 4,096
+// of 64 entries at K = 64 25.
 template <typename TV, int KC, int BS>
 __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
 {
@@ -514,7 +521,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
 }
 
 // Lists of the teacher's entries of 32 rows, those that the row allows, by blocks of candidates.  Order inside a block does not matter: every entry has a
-// place of its own in the tile of the candidates' kernel.
+// place of its own in the tile of the candidates' kernel.  16,384 x 32 entries 11 us, most of it the counts of 602 blocks.
 __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
 {
     extern __shared__ uint32_t place[];  // [entry_blocks]
@@ -565,7 +572,7 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
 constexpr int FIELD_ITEMS = 8192;                        // wavefronts that a sweep is split into, at most
 constexpr int64_t FIELD_GMAX_FLOATS = int64_t(1) << 26;  // maxima of groups held at a time; more rows take several rounds
 constexpr int64_t FIELD_MOST_ROWS = int64_t(1) << 22;    // rows to a launch of a workgroup each
-constexpr int64_t FIELD_WIDE_ROWS = 2048;                // below, a row gets a workgroup of four wavefronts, else one
+constexpr int64_t FIELD_WIDE_ROWS = 2048;                // below, a row gets a workgroup of four wavefronts, else one (8,191 rows 91 / 65 us)
 // Logits of a row in LDS, one kernel: V of up to so many values, rows of 16 of them at least, and up to so many rows.  us, one kernel /
 // several: 1 x 1,000 (K = 8) 9.9 / 17.3, 1 x 4,096 (K = 16) 11.7 / 17.4, 1 x 8,192 18.5 / 17.4, 256 x 4,096 14.2 / 21.8,
 // 512 x 1,000 9.9 / 22.2, 512 x 8,000 26.6 / 25.0.

@@ -14,7 +14,11 @@ __device__ __forceinline__ void wave_sync()
 // A wavefront takes 16 NT candidates and a part of the rows, 32 of them at a time.  The tiles of logits have rows down and
 // candidates across, so that they are the B operand of the second product (rows are what it sums over) as they stand:
 //   grad_V^T[k][j] += gs[i][k] P[i][j],   P_ij = 2^(x_ij - m_i) - (share of the teacher),   gs = weight scale / S G.
-// The teacher's few entries, none of them left out, come into the tiles by way of LDS.
+// The teacher's few entries, none of them left out, come into the tiles by way of LDS: 32 times as many entries cost nothing that
+// can be measured (16,384 x 38,461, K = 16, 1 and 32 entries to a row, 386 and 381 us).
+// Bound like k_field_rows_packed, with six products for grad_V whatever the type of V: 16,384 x 38,461, K = 16 380 to 445 us,
+// 4,096 x 100,001, K = 64 in bfloat16 530 to 575 (fp32 products 838 and 1430).  Four tiles of candidates in registers at K <= 16 (two
+// 471), two up to K = 64 (four spill, one 862).  Operands straight from the caches instead of by way of LDS: 493 and 1174.
 template <int KC>
 struct ColsShape {
     static constexpr int NG = FieldOps<3, KC>::NG, NG1 = FieldOps<1, KC>::NG;  // KC = 1: 2 operands of G against bfloat16 values
@@ -216,7 +220,7 @@ __global__ __launch_bounds__(64 * ColsShape<KC>::W, KC == 16 ? 1 : 2) void k_fie
     }
 }
 
-// The parts of grad_V and grad_w, added in the order of the rows.
+// The parts of grad_V and grad_w, added in the order of the rows.  Bound by the bytes: 3 x 100,001 x 64 32 us, 2.9 TB/s.
 __global__ __launch_bounds__(FM_BLOCK) void k_field_cols_sum(const FieldArgs A, int32_t KP)
 {
     const int64_t i = (int64_t)blockIdx.x * FM_BLOCK + threadIdx.x;

@@ -129,7 +129,10 @@ __device__ __forceinline__ void store_maxima(const FieldArgs& A, const float (&t
 // A wavefront takes 16 rows and a part of the candidates, 16 of them at a time.  The tile of logits has candidates down and
 // rows across, so that a lane has four candidates of one row: maxima and sums stay in the lane, and the tile is the B operand
 // of the second product (candidates are what it sums over) as it stands.  fp32 products straight from V: for calls with so
-// few rows that laying V out would cost more than it saves.  The wavefronts of a workgroup share the rows and the part.
+// few rows that laying V out would cost more than it saves.  The wavefronts of a workgroup share the rows and the part, so that
+// there are eight times fewer parts to join (1 x 1e6, K = 16: 8 to 1 wavefront 34 / 45 us a call).
+// Bound by the bytes of V where it is large: 3 x 4e6, K = 64 in fp32, 1.04 GB in 200 us, 5.2 TB/s.  1 x 1e6, K = 16 in half
+// precision takes 17 us for 36 MB: two round trips to memory of every wavefront, all of them at once.  64 x 38,461: 8 us.
 template <typename TV, int KC, int FILL, bool DISTILL>
 __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldArgs A)
 {
@@ -269,7 +272,8 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
     s.leave(A, split, row0, lo, g);
 }
 
-// Lays V and w out: a wavefront to 32 candidates.
+// Lays V and w out: a wavefront to 32 candidates.  Bound by what it writes, 48 bytes of operands for the logits and 96 more for
+// the sums of candidates to 16 values of a candidate in fp32: 100,001 x 64 in bfloat16 18 us, 38,461 x 16 in fp32 6.
 template <typename TV, int KC, int FILL, bool DISTILL>
 __global__ __launch_bounds__(FM_BLOCK) void k_field_pack(const FieldArgs A)
 {
@@ -325,6 +329,14 @@ __global__ __launch_bounds__(FM_BLOCK) void k_field_pack(const FieldArgs A)
 }
 
 // The same as k_field_rows from the packed table, products as sums of bfloat16 ones.
+// A block of 64 logits to a lane takes four vector instructions to each (scale and shift, exponential, its sum, the
+// entropy's sum) and half a one for the maximum, for distillation 5.5 more that split it into three parts; an exponential takes the
+// time of two.  The matrix instructions run beside those of other wavefronts only in part, so that the sum of both is
+// what bounds the kernel: 50,000 x 20,000, K = 16 275 to 300 us with vector instructions 75 % and matrix instructions 29 % of the
+// time (fp32 products took 527), 8,191 x 38,461, K = 64 in bfloat16 121 (461), distillation 16,384 x 38,461, K = 16 330 us, 73 and
+// 33 % (498), 4,096 x 100,001, K = 64 in bfloat16 310, 55 and 45 % (1142).  Products of two parts instead of three would save 17 % and
+// lose four bits.
+// The operands by way of LDS: distillation K = 64 355 us straight from the caches, 318; K = 16 no difference.
 template <int NP, int KC, bool DISTILL>
 struct RowsShape {
     static constexpr int NV = FieldOps<NP, KC>::NV, OPS = 4 * NV + (DISTILL ? 2 * KC * NP : 0);  // to a block of 64 candidates
