@@ -272,6 +272,76 @@ __global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_rows(const FieldA
     s.leave(A, split, row0, lo, g);
 }
 
+// One row against rows of V of LOADS times 16 bytes: a lane has a whole candidate, products on the vector units.  A matrix tile
+// would be empty but for this row, and a lane would ask for 8 bytes at a time where it asks for 16 to 64 here.  Bound by V and
+// two trips to memory.  10^6 candidates, K = 16, half precision: call 27.8 us, with matrix tiles 35.0; 10^6 of K = 8 in fp32
+// 26.7 and 36.5; 4*10^6 of K = 16 in fp32 63.1 and 66.5; 8,000 of K = 8 16.7 and 17.7.  Two rows in a lane's registers: 0.92
+// to 1.03 of the time with tiles, four 1.0 to 1.18, so only single rows come here.
+template <typename TV, int LOADS>
+__global__ __launch_bounds__(64 * FM_FIELD_SHARE) void k_field_row_one(const FieldArgs A)
+{
+    constexpr int W = FM_FIELD_SHARE, PER = 16 / sizeof(TV), K = LOADS * PER;
+    typedef TV Piece __attribute__((ext_vector_type(PER), aligned(sizeof(TV))));
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t beg = (int64_t)blockIdx.x * A.chunk, end = min(A.C, beg + A.chunk);
+    Piece next[LOADS];
+    float w_next = 0.f;
+    uint32_t bits_next = ~0u;
+    const auto ask = [&](int64_t j0) {
+        const int64_t j = min(j0 + lane, A.C - 1);
+        const TV* v = static_cast<const TV*>(A.V) + j * A.v_stride;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) next[i] = *reinterpret_cast<const Piece*>(v + i * PER);
+        if (A.w != nullptr) w_next = A.w[j];
+        if (A.mask != nullptr) bits_next = A.mask[j >> 5];
+    };
+    const int64_t first = beg + wave * FM_BLOCK_CANDS;
+    if (first < end) ask(first);
+    float g[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) g[k] = A.G[k];
+    float m = 0.5f * A.out * A.sl, S = 0.f, U = 0.f, best = A.out;  // m above all that is left out
+    for (int64_t j0 = first; j0 < end; j0 += W * FM_BLOCK_CANDS) {
+        float z = 0.f;
+#pragma unroll
+        for (int k = 0; k < K; ++k) z = fmaf(g[k], (float)next[k / PER][k % PER], z);
+        z = fmaxf_or_nan(fmaf(z, 0.f, z) + w_next, A.out);  // infinite values of G and V count as NaN
+        const bool there = j0 + lane < end && (bits_next >> (lane & 31) & 1u) != 0;
+        z = there ? z : A.out;
+        if (j0 + W * FM_BLOCK_CANDS < end) ask(j0 + W * FM_BLOCK_CANDS);
+        best = fmaxf(best, z);
+        if (A.gmax != nullptr) {
+            float x = fmaxf(z, fm_xor_lane<1>(z));
+            x = fmaxf(x, fm_xor_lane<2>(x));
+            x = fmaxf(x, fm_xor_lane<16>(x));
+            x = fmaxf(x, fm_xor_lane<32>(x));
+            if (lane < 16 && lane % 4 == 0) A.gmax[j0 / FM_BLOCK_CANDS * 4 + lane / 4] = x;
+        }
+        if (__any(z * A.sl > m + 8.f)) {
+            const float to = fmaxf(m, z * A.sl), d = m - to, f = __builtin_amdgcn_exp2f(d);
+            U = f > 0.f ? f * (U + d * S) : 0.f;
+            S *= f;
+            m = to;
+        }
+        const float x = fmaf(z, A.sl, -m), e = __builtin_amdgcn_exp2f(x);
+        S += e;
+        U = fmaf(e, x, U);
+    }
+    __shared__ float4 parts[W];
+    FieldPart p = fm_field_wave_merge({m, S, U});
+    for (int x = 32; x > 0; x >>= 1) best = fmaxf(best, __shfl_xor(best, x));
+    if (lane == 0) parts[wave] = make_float4(p.m, p.S, p.U, best);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    p = {-INFINITY, 0.f, 0.f};
+    float most = -INFINITY;
+    for (int i = 0; i < W; ++i) {
+        p = fm_field_merge(p, {parts[i].x, parts[i].y, parts[i].z});
+        most = fmaxf(most, parts[i].w);
+    }
+    A.part[blockIdx.x] = make_float4(p.m, p.S, p.U, most);
+}
+
 // Lays V and w out: a wavefront to 32 candidates.  Bound by what it writes, 48 bytes of operands for the logits and 96 more for
 // the sums of candidates to 16 values of a candidate in fp32: 100,001 x 64 in bfloat16 18 us, 38,461 x 16 in fp32 6.
 template <typename TV, int KC, int FILL, bool DISTILL>
@@ -471,9 +541,27 @@ void rows_kernel(bool packed, int32_t v_type, int32_t K, F run)
     });
 }
 
+// 16-byte pieces to a row of V in calls that k_field_row_one takes, else 0.
+int one_loads(int32_t v_type, const FieldArgs& A)
+{
+    const int bytes = A.K * (v_type == FM_TYPE_F32 ? 4 : 2);
+    return !A.packed && A.n == 1 && (bytes == 16 || bytes == 32 || bytes == 64) ? bytes / 16 : 0;
+}
+
+template <typename TV>
+void row_one(int loads, const FieldArgs& A, hipStream_t st)
+{
+    const auto kernel = loads == 1 ? k_field_row_one<TV, 1> : loads == 2 ? k_field_row_one<TV, 2> : k_field_row_one<TV, 4>;
+    kernel<<<(uint32_t)A.splits, 64 * FM_FIELD_SHARE, 0, st>>>(A);
+}
+
 template <bool DISTILL>
 void rows(int32_t v_type, const FieldArgs& A, hipStream_t st)
 {
+    if (const int loads = DISTILL ? 0 : one_loads(v_type, A)) {
+        if (v_type == FM_TYPE_F32) return row_one<float>(loads, A, st);
+        return v_type == FM_TYPE_F16 ? row_one<_Float16>(loads, A, st) : row_one<__bf16>(loads, A, st);
+    }
     rows_kernel<DISTILL>(A.packed, v_type, A.K, [&](auto kernel, auto pack, int waves, size_t lds) {
         if (A.packed) {
             pack<<<blocks_of(A.blocks * 2), FM_BLOCK, 0, st>>>(A);

@@ -479,6 +479,18 @@ def test_from_the_packed_table(n, C, K, T, vtype, mask):
     _check_distill(_run_distill(d, 0.6), d, 0.6)
 
 
+@pytest.mark.parametrize("n", [1, 2, 3, 4])
+@pytest.mark.parametrize("C,K,vtype", [(70_001, 16, "float16"), (30_000, 16, "float32"), (9_999, 8, "float32"), (40_003, 8, "bfloat16"),
+                                       (25_000, 32, "bfloat16"), (66_000, 4, "float32"), (33_333, 64, "float16")])
+def test_few_rows_of_a_large_field(n, C, K, vtype):
+    print("few", n, C, K, vtype, flush=True)
+    for mask in ("none", "shared", "rows"):
+        d = _data(n + C, n, C, K, 3, vtype, mask, True)
+        _check_logprobs(_run_logprobs(d, 1.0, 10), d, 1.0, 10)
+        d = _data(n + C, n, C, K, 3, vtype, mask, False)
+        _check_logprobs(_run_logprobs(d, 0.7, 0), d, 0.7, 0)
+
+
 def test_every_row_names_the_same_candidates():
     """More entries in a block of candidates than lanes, and all of them at the same few candidates."""
     d = _data(31, 500, 9_000, 16, 40, "float32", "none", False)
