@@ -283,7 +283,7 @@ int fm_field_logprobs(fm_field* f, const fm_candidates* c, int64_t n, const floa
 
 /* Distillation from a teacher's T largest logits of every row, 1 <= T <= max_entries, n <= 2^22; entries with ids outside [0, C),
  * such that the row does not allow and with a logit of -infinity are left out, the ids of a row are distinct (the shares
- * of equal ones add up).
+ * of equal ones add up, of three or more in an order that may differ from call to call).
  *   q_it   = softmax over the entries of a row of scale * teacher_it
  *   loss_i = sum_t q_it (log q_it - log p_{i, ids_it})               (Kullback-Leibler; T = 1: cross entropy of a label)
  * and the gradient of sum_i weight_i loss_i (weight NULL: ones), with d_ij = weight_i scale (p_ij - q_ij):

@@ -521,7 +521,7 @@ __global__ __launch_bounds__(BS) void k_field_distill_rows(const FieldArgs A)
 }
 
 // Lists of the teacher's entries of 32 rows, those that the row allows, by blocks of candidates.  Order inside a block does not matter: every entry has a
-// place of its own in the tile of the candidates' kernel.  16,384 x 32 entries 11 us, most of it the counts of 602 blocks.
+// place of its own in the tile of the candidates' kernel, equal ids of a row aside.  16,384 x 32 entries 11 us, most of it the counts of 602 blocks.
 __global__ __launch_bounds__(FM_BLOCK) void k_field_entries(const FieldArgs A)
 {
     extern __shared__ uint32_t place[];  // [entry_blocks]
